@@ -397,6 +397,127 @@ int sage_attn_clock_debug(const int8_t* q_i8, const float* q_scale, const int8_t
 int sage_microbench(int kind, int waves_per_simd, int workgroups, int iters,
                     const int32_t* data, uint64_t* out, void* stream);
 
+/*
+ * ---- Serving: rotary positions, and a cache of K and V held in 4 bits
+ *
+ * Tensors of these calls are [B, H, N, D] with the channels next to each other and, where a `*_strides` argument is given,
+ * any distances between batches, heads and tokens: a host pointer to those three strides in elements, or NULL for a
+ * contiguous tensor.  Every row starts on a 16-byte boundary (SAGE_ERR_ALIGN), and rows that are written are not each other's
+ * memory.  `type` is one of the three constants below.
+ */
+enum { SAGE_F16 = 0, SAGE_BF16 = 1, SAGE_F32 = 2 };
+
+/*
+ * Rotary positions (Section 4.6 names them as the producer of Q and K) by themselves, of one tensor or of two in one launch:
+ * pair i of the first `rotated` channels is turned by the angle position * inv_freq[i],
+ *     y0 = x0 c - x1 s,   y1 = x1 c + x0 s,   c = amplitude cos(angle), s = amplitude sin(angle),
+ * the angle reduced in fp64, products and sum in fp32, one rounding to the tensor's type; the other channels are copied.
+ *   interleaved     0: pair i is channels i and i + rotated / 2;  non-zero: channels 2 i and 2 i + 1
+ *   q, k            in   [B,Hq,N,D] and [B,Hk,N,D];  q_out, k_out  out, the same tensors or others (not overlapping otherwise);
+ *                   k and k_out NULL and Hk = 0 for one tensor
+ *   positions       in   int32; token n of sequence b is at positions[b * position_stride + n] (0: shared by all)
+ *   inv_freq        in   [rotated / 2] fp64, radians per position: where a context is scaled, the scaled ones
+ *   amplitude       multiplies the rotated channels (1; some scalings of the context use another); finite
+ *   D a multiple of 8 up to 512, rotated even, 2 .. D; type SAGE_F16, SAGE_BF16 or SAGE_F32; B * (Hq + Hk) at most 65535
+ * sage_rope_bwd takes the gradient of the outputs to the gradient of the inputs: the turn back, times amplitude.
+ */
+int sage_rope(const void* q, const int64_t* q_strides, void* q_out, const int64_t* q_out_strides,
+              const void* k, const int64_t* k_strides, void* k_out, const int64_t* k_out_strides,
+              const int32_t* positions, int64_t position_stride, const double* inv_freq, float amplitude,
+              int B, int Hq, int Hk, int N, int D, int rotated, int type, int interleaved, void* stream);
+int sage_rope_bwd(const void* dq, const int64_t* dq_strides, void* dq_out, const int64_t* dq_out_strides,
+                  const void* dk, const int64_t* dk_strides, void* dk_out, const int64_t* dk_out_strides,
+                  const int32_t* positions, int64_t position_stride, const double* inv_freq, float amplitude,
+                  int B, int Hq, int Hk, int N, int D, int rotated, int type, int interleaved, void* stream);
+
+/*
+ * The cache: a pool [num_pages, Hkv, block] of bytes, block = sage_cache4_block_bytes(), each page `page` tokens of all heads,
+ * and per sequence a row of the table `pages` [B, columns] int32: token slot s of sequence b lies in page
+ * pages[b][s / page], row s % page.  An entry outside 0 .. num_pages - 1 holds no tokens: what is stored there is dropped, what
+ * is read there is absent (no key for the attention, zeros for sage_cache4_load).  Pages that a call writes belong to one
+ * sequence each.  Per token, head and group of channels Section 3.2's quantizer with 7 in place of 127,
+ *     delta = fp16(min(amax / 7, 65504)),  code = clamp(round_half_even(x / delta), -7, 7)   (fp32 divisions; delta = 0: 0),
+ * where x is V, or fp32(K) - k_mean (Section 4.2: the attention does not change with a vector added to all keys of a head,
+ * and K's channels carry a large one, which 4 bits have no room for).  A NaN is stored as 0, infinities as the largest value.
+ * Inside a block: K codes [page][D/2], V codes [page][D/2], K scales [page][D/group], V scales [page][D/group]; a code is the
+ * nibble code + 8; V's in the order of the channels, low nibble first; K's row holds channel 32 i + 8 h + e in 32-bit word
+ * h * D / 32 + i, nibble e / 2 + 4 (e % 2).
+ *   page   16, 32, 64, 128 or 256;  group  32, 64 or 128, at most D;  D  64 or 128;  columns * page at most 2^23
+ * sage_cache4_block_bytes returns 0 for a form that is not covered.
+ */
+size_t sage_cache4_block_bytes(int D, int page, int group);
+
+/*
+ * New tokens into the cache: token n < count[b] of sequence b goes to slot start[b] + n; a slot outside the table is dropped.
+ *   k, v    in   [B,Hkv,N,D] SAGE_F16 or SAGE_BF16
+ *   k_mean  in   [B,Hkv,D] fp32, 16-byte aligned, or NULL: subtracted from K.  The same one for all tokens of a sequence.
+ *   cache   in/out; everything but the tokens' rows is left as it was
+ *   start   in   [B] int32;  count  in  [B] int32, or NULL: N
+ */
+int sage_cache4_append(const void* k, const int64_t* k_strides, const void* v, const int64_t* v_strides, const float* k_mean,
+                       void* cache, const int32_t* pages, const int32_t* start, const int32_t* count,
+                       int B, int Hkv, int N, int D, int type, int num_pages, int columns, int page, int group, void* stream);
+
+/*
+ * Tokens read back: row n of k and v [B,Hkv,N,D] (out, contiguous) is slot start[b] + n (start NULL: n), as the values that its
+ * codes stand for, plus k_mean for K if it is given; zeros for n >= count[b] and for slots that hold no token.
+ */
+int sage_cache4_load(const void* cache, const int32_t* pages, const int32_t* start, const int32_t* count, const float* k_mean,
+                     void* k, void* v, int B, int Hkv, int N, int D, int type, int num_pages, int columns, int page, int group,
+                     void* stream);
+
+/*
+ * Attention of new queries over the cache, softmax(sm_scale q K^T) V with K and V as the cache holds them: FP16 products of the
+ * codes with fp32 accumulation (q is not quantized), the scales applied to the sums.  Query head hq reads key head
+ * hq / (Hq / Hkv).
+ *   q        in   [B,Hq,Nq,D] SAGE_F16 or SAGE_BF16;  out  out, the same type and shape, fully overwritten
+ *   lengths  in   [B] int32: tokens of the sequence in the cache (the queries' own among them); limited to 0 .. columns * page
+ *   count    in   [B] int32, or NULL: Nq.  Sequence b has the queries t < count[b]; the rows behind them become zeros
+ *   causal   non-zero: query t sees slots up to lengths[b] - count[b] + t;  0: all of lengths[b].  A query that sees
+ *            no key has the output 0
+ *   lse      out  [B,Hq,Nq] fp32, or NULL: ln of the sum of exp(sm_scale q K^T), -infinity without a key.  (K as the cache holds
+ *            it: a k_mean moves it by sm_scale q . k_mean)
+ *   n_splits   how many workgroups share a row's keys, 0: chosen from the shape
+ *   workspace  device, >= sage_cache4_attn_workspace() bytes (same arguments), 16-byte aligned; scratch, contents undefined
+ *              on entry and exit; may be NULL when that size is 0.  Two calls that share one are ordered by the caller
+ */
+size_t sage_cache4_attn_workspace(int B, int Hq, int Hkv, int Nq, int D, int columns, int page, int n_splits);
+int sage_cache4_attn(const void* q, const int64_t* q_strides, const void* cache, const int32_t* pages, const int32_t* lengths,
+                     const int32_t* count, void* out, const int64_t* out_strides, float* lse, void* workspace, size_t workspace_bytes,
+                     int B, int Hq, int Hkv, int Nq, int D, int type, int num_pages, int columns, int page, int group, int causal,
+                     float sm_scale, int n_splits, void* stream);
+
+/*
+ * The weight that the queries of such a call gave to each key, added to what it had:
+ *     out[b][h][s] = weights[b][h][s] + sum over the query heads of key head h and the queries that see slot s of
+ *                                       exp(sm_scale q K^T - lse),
+ * the sum in fp32, in an order that does not change from call to call.
+ *   lse      in   from sage_cache4_attn with the same arguments (a row whose lse is -infinity adds nothing)
+ *   weights  in   [B,Hkv,width] fp32, or NULL: zeros;  out  out, the same shape, may be weights itself; width >= columns * page.
+ *            Slots from lengths[b] on keep their value
+ */
+int sage_cache4_weights(const void* q, const int64_t* q_strides, const void* cache, const int32_t* pages, const int32_t* lengths,
+                        const int32_t* count, const float* lse, const float* weights, float* out, int width,
+                        int B, int Hq, int Hkv, int Nq, int D, int type, int num_pages, int columns, int page, int group, int causal,
+                        float sm_scale, void* stream);
+
+/*
+ * The least used tokens left behind: of the lengths[b] tokens of a sequence every head keeps the last `recent` and, of those
+ * before them, the keep - recent with the largest weights (of equal ones the lowest slots; a NaN is less than any number), all
+ * of them where there are no more than keep.  Their rows are copied, in order, to slots 0, 1, ... of the pages in out_pages; the
+ * old pages are only read.  Heads of a sequence keep tokens of their own.
+ *   out_cache, out_num_pages   the pool of the new pages: the same pool or another one of the same form;  out_pages
+ *            [B, out_columns], none of them a page that `pages` names, out_columns * page >= keep
+ *   weights  in   [B,Hkv,width];  out_weights  out  [B,Hkv,out_width], out_width >= keep: the kept tokens' weights, then zeros
+ *   kept     out  [B,Hkv,keep] int32: the slots that were kept, ascending, then -1
+ *   out_lengths  out  [B] int32: min(lengths[b], keep)
+ *   keep >= 1, 0 <= recent <= keep;  SAGE_ERR_VALUE where an output is the input it is made from
+ */
+int sage_cache4_evict(const void* cache, int num_pages, const int32_t* pages, int columns, const int32_t* lengths,
+                      const float* weights, int width, void* out_cache, int out_num_pages, const int32_t* out_pages, int out_columns,
+                      float* out_weights, int out_width, int32_t* kept, int32_t* out_lengths,
+                      int B, int Hkv, int D, int page, int group, int keep, int recent, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -37,3 +37,15 @@ from .binding import (  # noqa: F401
     sage_status_string,
     sageattn,
 )
+from .serving import (  # noqa: F401
+    sage_cache4_append,
+    sage_cache4_attn,
+    sage_cache4_attn_workspace,
+    sage_cache4_block_bytes,
+    sage_cache4_evict,
+    sage_cache4_load,
+    sage_cache4_weights,
+    sage_rope,
+    sage_rope_bwd,
+    sage_rope_frequencies,
+)

@@ -29,7 +29,9 @@ EXPORTS = ("sage_status_string", "sage_source_hash", "sage_default_sm_scale", "s
            "sage_quant_v_workspace", "sage_quant_v_pitch", "sage_quant_v", "sage_attn_pv_int8_fwd",
            "sage_attn_cross_fwd", "sage_attn_pv_int8_cross_fwd",
            "sage_attn_split_count", "sage_attn_split_workspace", "sage_attn_cross_split_fwd",
-           "sage_attn_pv_int8_cross_split_fwd", "sage_attention_workspace", "sage_attention_fwd", "sage_microbench")
+           "sage_attn_pv_int8_cross_split_fwd", "sage_attention_workspace", "sage_attention_fwd", "sage_microbench",
+           "sage_rope", "sage_rope_bwd", "sage_cache4_block_bytes", "sage_cache4_append", "sage_cache4_load",
+           "sage_cache4_attn_workspace", "sage_cache4_attn", "sage_cache4_weights", "sage_cache4_evict")
 
 
 class SageError(RuntimeError):
@@ -121,6 +123,24 @@ def load() -> ctypes.CDLL:
     lib.sage_attention_fwd.argtypes = [c_void_p] * 5 + [c_size_t] + [c_int] * 6 + [c_float, c_int, c_int, c_int, c_void_p]
     lib.sage_microbench.restype = c_int
     lib.sage_microbench.argtypes = [c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p]
+    for name in ("sage_rope", "sage_rope_bwd"):
+        f = getattr(lib, name)
+        f.restype, f.argtypes = c_int, [c_void_p] * 9 + [ctypes.c_int64, c_void_p, c_float] + [c_int] * 8 + [c_void_p]
+    lib.sage_cache4_block_bytes.restype = c_size_t
+    lib.sage_cache4_block_bytes.argtypes = [c_int] * 3
+    lib.sage_cache4_append.restype = c_int
+    lib.sage_cache4_append.argtypes = [c_void_p] * 9 + [c_int] * 9 + [c_void_p]
+    lib.sage_cache4_load.restype = c_int
+    lib.sage_cache4_load.argtypes = [c_void_p] * 7 + [c_int] * 9 + [c_void_p]
+    lib.sage_cache4_attn_workspace.restype = c_size_t
+    lib.sage_cache4_attn_workspace.argtypes = [c_int] * 8
+    lib.sage_cache4_attn.restype = c_int
+    lib.sage_cache4_attn.argtypes = [c_void_p] * 10 + [c_size_t] + [c_int] * 11 + [c_float, c_int, c_void_p]
+    lib.sage_cache4_weights.restype = c_int
+    lib.sage_cache4_weights.argtypes = [c_void_p] * 9 + [c_int] * 12 + [c_float, c_void_p]
+    lib.sage_cache4_evict.restype = c_int
+    lib.sage_cache4_evict.argtypes = ([c_void_p, c_int, c_void_p, c_int, c_void_p, c_void_p, c_int] + [c_void_p, c_int, c_void_p, c_int, c_void_p, c_int]
+                                      + [c_void_p, c_void_p] + [c_int] * 7 + [c_void_p])
     _open_native(lib)
     _lib = lib
     return lib

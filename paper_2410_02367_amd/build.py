@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsage.so")
 SOURCES = ["sage_api.hip", "sage_prepass.hip", "sage_prepass_v.hip", "sage_attn.hip", "sage_attn_pv8.hip",
-           "sage_decode.hip", "sage_short.hip", "sage_microbench.hip"]
+           "sage_decode.hip", "sage_short.hip", "sage_microbench.hip", "sage_serving_api.hip", "sage_rope.hip", "sage_cache4.hip",
+           "sage_cache4_attn.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

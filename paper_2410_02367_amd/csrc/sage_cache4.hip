@@ -1,0 +1,286 @@
+// The cache held in 4 bits: tokens quantized into their pages, read back, and the least used ones left behind.
+//
+// The quantizer is Section 3.2's with 7 in place of 127, one scale per token, head and group of channels:
+//   delta = fp16(amax / 7),  code = clamp(round_half_even(x / delta), -7, 7),
+// the division by the scale as it is stored, so that the code is the nearest one for the reader.  x is v, or k - k_mean (Section
+// 4.2: a vector added to every key of a head does not change the softmax, and K's channels carry large ones).
+#include "sage_serving.h"
+#include "sage_device.h"
+
+namespace sage {
+
+namespace {
+constexpr float MAX_SCALE = 65504.0f;       // fp16's largest: values beyond 7 of it saturate
+
+// 8 channels of a row as fp32
+template <int TYPE>
+__device__ __forceinline__ void row8(const void* p, long at, float (&x)[8]) {
+    if constexpr (TYPE == TYPE_F16) {
+        const half8 v = *(const half8*)((const _Float16*)p + at);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+    } else {
+        typedef unsigned u4 __attribute__((ext_vector_type(4)));
+        const u4 v = *(const u4*)((const unsigned short*)p + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[2 * e] = __builtin_bit_cast(float, v[e] << 16);
+            x[2 * e + 1] = __builtin_bit_cast(float, v[e] & 0xffff0000u);
+        }
+    }
+}
+template <int TYPE>
+__device__ __forceinline__ void put_row8(void* p, long at, const float (&x)[8]) {
+    if constexpr (TYPE == TYPE_F16) {
+        half8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (_Float16)x[e];
+        *(half8*)((_Float16*)p + at) = v;
+    } else {
+        typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+        b8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (__bf16)x[e];
+        *(b8*)((__bf16*)p + at) = v;
+    }
+}
+// the scale of a group from its largest magnitude
+__device__ __forceinline__ _Float16 scale_of(float amax) { return (_Float16)__builtin_fminf(amax / 7.0f, MAX_SCALE); }
+// nibble of x; a NaN is stored as 0, infinities saturate
+__device__ __forceinline__ unsigned nibble(float x, float delta) {
+    const float c = __builtin_rintf(x / delta);
+    const float r = __builtin_fminf(__builtin_fmaxf(c, -7.0f), 7.0f);
+    return delta > 0.0f && x == x ? (unsigned)((int)r + 8) : 8u;
+}
+// where channel e of 8 stands in its word
+template <bool IS_K> __device__ __forceinline__ int nibble_shift(int e) { return IS_K ? 4 * (e >> 1) + 16 * (e & 1) : 4 * e; }
+// the word of octet o (channels 8 o .. 8 o + 7) in its row
+template <bool IS_K> __device__ __forceinline__ int octet_word(int o, int D) { return IS_K ? (o & 3) * (D / 32) + (o >> 2) : o; }
+
+template <int GROUP>
+__device__ __forceinline__ float group_max(const float (&x)[8]) {
+    float m = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = __builtin_fmaxf(m, __builtin_fabsf(x[e]));
+    return lanes_max<GROUP / 8>(m);
+}
+template <bool IS_K>
+__device__ __forceinline__ unsigned pack8(const float (&x)[8], float delta) {
+    unsigned w = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w |= nibble(x[e], delta) << nibble_shift<IS_K>(e);
+    return w;
+}
+template <bool IS_K>
+__device__ __forceinline__ void unpack8(unsigned w, float delta, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)((int)(w >> nibble_shift<IS_K>(e) & 15u) - 8) * delta;
+}
+}  // namespace
+
+// A thread takes 8 channels of K and of V of a token, D / 8 adjacent threads the token's row.
+template <int D, int GROUP, int TYPE>
+__global__ void __launch_bounds__(256) cache4_append_kernel(Cache4 c, const void* __restrict__ k, RowStrides ks, const void* __restrict__ v,
+                                                            RowStrides vs, const float* __restrict__ k_mean, const int* __restrict__ start,
+                                                            const int* __restrict__ count, int N) {
+    constexpr int OCTETS = D / 8, ROWS = 256 / OCTETS;
+    const int o = threadIdx.x % OCTETS, bh = blockIdx.y, b = bh / c.heads, h = bh - b * c.heads;
+    const int n = blockIdx.x * ROWS + threadIdx.x / OCTETS;
+    const int there = count != nullptr ? min(count[b], N) : N;
+    // (a row's threads stay or leave together: group_max looks at no other row's)
+    if (n >= there) return;
+    const long slot = (long)start[b] + n;
+    if (slot < 0 || slot >= c.capacity()) return;
+    unsigned char* block = c.block(b, h, (int)slot);
+    if (block == nullptr) return;
+    const int r = (int)slot & (c.page() - 1);
+    float x[8], y[8];
+    row8<TYPE>(k, b * ks.b + h * ks.h + n * ks.n + 8 * o, x);
+    row8<TYPE>(v, b * vs.b + h * vs.h + n * vs.n + 8 * o, y);
+    if (k_mean != nullptr) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] -= k_mean[(size_t)bh * D + 8 * o + e];
+    }
+    const _Float16 dk = scale_of(group_max<GROUP>(x)), dv = scale_of(group_max<GROUP>(y));
+    ((unsigned*)(block + c.k_codes(r)))[octet_word<true>(o, D)] = pack8<true>(x, (float)dk);
+    ((unsigned*)(block + c.v_codes(r)))[octet_word<false>(o, D)] = pack8<false>(y, (float)dv);
+    if (o % (GROUP / 8) == 0) {
+        ((_Float16*)(block + c.k_scales(r)))[o / (GROUP / 8)] = dk;
+        ((_Float16*)(block + c.v_scales(r)))[o / (GROUP / 8)] = dv;
+    }
+}
+
+template <int D, int GROUP, int TYPE>
+__global__ void __launch_bounds__(256) cache4_load_kernel(Cache4 c, const int* __restrict__ start, const int* __restrict__ count,
+                                                          const float* __restrict__ k_mean, void* __restrict__ k, void* __restrict__ v, int N) {
+    constexpr int OCTETS = D / 8, ROWS = 256 / OCTETS;
+    const int o = threadIdx.x % OCTETS, bh = blockIdx.y, b = bh / c.heads, h = bh - b * c.heads;
+    const int n = blockIdx.x * ROWS + threadIdx.x / OCTETS;
+    if (n >= N) return;
+    const int there = count != nullptr ? min(count[b], N) : N;
+    const long slot = (start != nullptr ? (long)start[b] : 0l) + n;
+    const unsigned char* block = n < there && slot >= 0 && slot < c.capacity() ? c.block(b, h, (int)slot) : nullptr;
+    float x[8] = {}, y[8] = {};
+    if (block != nullptr) {
+        const int r = (int)slot & (c.page() - 1);
+        unpack8<true>(((const unsigned*)(block + c.k_codes(r)))[octet_word<true>(o, D)],
+                      (float)((const _Float16*)(block + c.k_scales(r)))[o / (GROUP / 8)], x);
+        unpack8<false>(((const unsigned*)(block + c.v_codes(r)))[octet_word<false>(o, D)],
+                       (float)((const _Float16*)(block + c.v_scales(r)))[o / (GROUP / 8)], y);
+        if (k_mean != nullptr) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] += k_mean[(size_t)bh * D + 8 * o + e];
+        }
+    }
+    const long at = ((long)bh * N + n) * D + 8 * o;
+    put_row8<TYPE>(k, at, x);
+    put_row8<TYPE>(v, at, y);
+}
+
+#define SAGE_CACHE4_SHAPE(KERNEL, TYPE, ...)                                                                       \
+    do {                                                                                                            \
+        if (c.D == 64 && c.group == 32) KERNEL<64, 32, TYPE><<<grid, 256, 0, st>>>(__VA_ARGS__);                    \
+        else if (c.D == 64) KERNEL<64, 64, TYPE><<<grid, 256, 0, st>>>(__VA_ARGS__);                                \
+        else if (c.group == 32) KERNEL<128, 32, TYPE><<<grid, 256, 0, st>>>(__VA_ARGS__);                           \
+        else if (c.group == 64) KERNEL<128, 64, TYPE><<<grid, 256, 0, st>>>(__VA_ARGS__);                           \
+        else KERNEL<128, 128, TYPE><<<grid, 256, 0, st>>>(__VA_ARGS__);                                             \
+    } while (0)
+
+hipError_t launch_cache4_append(const Cache4& c, const void* k, const RowStrides& ks, const void* v, const RowStrides& vs,
+                                const float* k_mean, const int* start, const int* count, int B, int N, int type, hipStream_t st) {
+    const int rows = 256 / (c.D / 8);
+    const dim3 grid((N + rows - 1) / rows, B * c.heads);
+    if (type == TYPE_BF16) SAGE_CACHE4_SHAPE(cache4_append_kernel, TYPE_BF16, c, k, ks, v, vs, k_mean, start, count, N);
+    else SAGE_CACHE4_SHAPE(cache4_append_kernel, TYPE_F16, c, k, ks, v, vs, k_mean, start, count, N);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache4_load(const Cache4& c, const int* start, const int* count, const float* k_mean, void* k, void* v, int B, int N,
+                              int type, hipStream_t st) {
+    const int rows = 256 / (c.D / 8);
+    const dim3 grid((N + rows - 1) / rows, B * c.heads);
+    if (type == TYPE_BF16) SAGE_CACHE4_SHAPE(cache4_load_kernel, TYPE_BF16, c, start, count, k_mean, k, v, N);
+    else SAGE_CACHE4_SHAPE(cache4_load_kernel, TYPE_F16, c, start, count, k_mean, k, v, N);
+    return hipGetLastError();
+}
+
+// ---- eviction
+// The slots that stay, in order: the last `recent` of n and, of the m before them, the need = keep - recent with the largest
+// weights, of equal ones the lowest slots.  One workgroup per (sequence, head).  The need-th largest weight is found a byte at
+// a time from the top (a histogram of the weights that share the bytes found so far); then every wavefront counts, in a share
+// of the slots of its own, those above it and those equal to it, and writes its share.
+namespace {
+// larger weight, larger key; a NaN below all numbers, -0 with 0
+__device__ __forceinline__ unsigned rank_key(float w) {
+    const unsigned u = __builtin_bit_cast(unsigned, w + 0.0f);
+    return w != w ? 0u : (u >> 31 ? ~u : u | 0x80000000u);
+}
+}  // namespace
+
+constexpr int SELECT_NT = 1024, SELECT_WAVES = SELECT_NT / 64;
+__global__ void __launch_bounds__(SELECT_NT) cache4_select_kernel(const int* __restrict__ lengths, const float* __restrict__ weights, int width,
+                                                                  int capacity, int heads, int* __restrict__ kept,
+                                                                  int* __restrict__ out_lengths, int keep, int recent) {
+    __shared__ int histogram[256];
+    __shared__ int s_digit, s_above, s_gt[SELECT_WAVES], s_eq[SELECT_WAVES];
+    const int bh = blockIdx.x, b = bh / heads, t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int n = min(max(lengths[b], 0), capacity);
+    int* const to = kept + (size_t)bh * keep;
+    if (bh == b * heads && t == 0) out_lengths[b] = min(n, keep);
+    if (n <= keep) {
+        for (int i = t; i < keep; i += SELECT_NT) to[i] = i < n ? i : -1;
+        return;
+    }
+    const float* const w = weights + (size_t)bh * width;
+    const int m = n - recent, need = keep - recent;
+    for (int i = t; i < recent; i += SELECT_NT) to[need + i] = m + i;
+    if (need == 0) return;
+    unsigned found = 0, mask = 0;
+    int left = need;                    // of the keys that match `found` under `mask`, how many stay
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        if (t < 256) histogram[t] = 0;
+        __syncthreads();
+        for (int i = t; i < m; i += SELECT_NT) {
+            const unsigned u = rank_key(w[i]);
+            if ((u & mask) == found) atomicAdd(&histogram[u >> shift & 255u], 1);
+        }
+        __syncthreads();
+        if (t == 0) {
+            int above = 0, d = 255;
+            while (d > 0 && above + histogram[d] < left) above += histogram[d--];
+            s_digit = d;
+            s_above = above;
+        }
+        __syncthreads();
+        found |= (unsigned)s_digit << shift;
+        mask |= 255u << shift;
+        left -= s_above;
+    }
+    const int share = (m + SELECT_WAVES * 64 - 1) / (SELECT_WAVES * 64) * 64, first = min(wave * share, m), last = min(first + share, m);
+    int gt = 0, eq = 0;
+    for (int i = first + lane; i - lane < last; i += 64) {
+        const unsigned u = i < last ? rank_key(w[i]) : 0u;
+        gt += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < last && u > found));
+        eq += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < last && u == found));
+    }
+    if (lane == 0) {
+        s_gt[wave] = gt;
+        s_eq[wave] = eq;
+    }
+    __syncthreads();
+    int at = 0, ties = 0;               // slots written, equal ones seen before this share
+    for (int i = 0; i < wave; ++i) {
+        at += s_gt[i];
+        ties += s_eq[i];
+    }
+    at += min(ties, left);
+    for (int i = first + lane; i - lane < last; i += 64) {
+        const unsigned u = i < last ? rank_key(w[i]) : 0u;
+        const unsigned long long equal = __builtin_amdgcn_ballot_w64(i < last && u == found), below = (1ull << lane) - 1ull;
+        const bool stays = i < last && (u > found || (u == found && ties + __builtin_popcountll(equal & below) < left));
+        const unsigned long long all = __builtin_amdgcn_ballot_w64(stays);
+        if (stays) to[at + __builtin_popcountll(all & below)] = i;
+        at += __builtin_popcountll(all);
+        ties += __builtin_popcountll(equal);
+    }
+}
+
+// The kept rows copied: D / 32 threads for 16 bytes each of the K codes, as many for V's; each also one of the 2 D / group
+// scales.  A row whose page holds no tokens becomes zeros.
+template <int D>
+__global__ void __launch_bounds__(256) cache4_gather_kernel(Cache4 c, Cache4 to, const int* __restrict__ kept, const float* __restrict__ weights,
+                                                            int width, float* __restrict__ out_weights, int out_width, int keep) {
+    constexpr int TPR = D / 16, ROWS = 256 / TPR;
+    typedef unsigned u4 __attribute__((ext_vector_type(4)));
+    const int bh = blockIdx.y, b = bh / c.heads, h = bh - b * c.heads, i = threadIdx.x % TPR;
+    const int j = blockIdx.x * ROWS + threadIdx.x / TPR;
+    const int from = j < keep ? kept[(size_t)bh * keep + j] : -1;
+    if (i == 0 && j < out_width) out_weights[(size_t)bh * out_width + j] = from >= 0 ? weights[(size_t)bh * width + from] : 0.0f;
+    if (from < 0) return;
+    unsigned char* const dst = to.block(b, h, j);
+    if (dst == nullptr) return;
+    const unsigned char* const src = c.block(b, h, from);
+    const int rs = from & (c.page() - 1), rd = j & (to.page() - 1), S = c.scales();
+    const bool is_v = i >= TPR / 2;
+    const int chunk = is_v ? i - TPR / 2 : i;
+    const u4 x = src != nullptr ? ((const u4*)(src + (is_v ? c.v_codes(rs) : c.k_codes(rs))))[chunk]
+                                : (u4){0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u};
+    ((u4*)(dst + (is_v ? to.v_codes(rd) : to.k_codes(rd))))[chunk] = x;
+    if (chunk < S) {
+        const unsigned short s = src != nullptr ? ((const unsigned short*)(src + (is_v ? c.v_scales(rs) : c.k_scales(rs))))[chunk] : 0;
+        ((unsigned short*)(dst + (is_v ? to.v_scales(rd) : to.k_scales(rd))))[chunk] = s;
+    }
+}
+
+hipError_t launch_cache4_evict(const Cache4& c, const int* lengths, const float* weights, int width, const Cache4& to, float* out_weights,
+                               int out_width, int* kept, int* out_lengths, int B, int keep, int recent, hipStream_t st) {
+    cache4_select_kernel<<<B * c.heads, SELECT_NT, 0, st>>>(lengths, weights, width, c.capacity(), c.heads, kept, out_lengths, keep, recent);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    const int rows = 256 / (c.D / 16);
+    const dim3 grid((out_width + rows - 1) / rows, B * c.heads);
+    if (c.D == 64) cache4_gather_kernel<64><<<grid, 256, 0, st>>>(c, to, kept, weights, width, out_weights, out_width, keep);
+    else cache4_gather_kernel<128><<<grid, 256, 0, st>>>(c, to, kept, weights, width, out_weights, out_width, keep);
+    return hipGetLastError();
+}
+
+}  // namespace sage
