@@ -4,115 +4,617 @@
 //   weights[key] += sum over the queries of the key's heads of exp(S - lse).
 //
 // Query t of the n that a sequence has is its token number length - n + t; with the causal mask it sees the tokens up to itself.
+//
+// One pass over the cache.  A row is a (query, head of the key head's group) pair, row t * share + g; a workgroup takes 16 QT rows
+// of one (sequence, key head) and its four wavefronts take tiles of 64 keys in turn, each with its own running reference, sum
+// and O, without a barrier, and add up at the end; long caches are cut into chunks for several workgroups and merged.
+//
+// Codes go to the matrix pipe as they are, scales are applied to sums.  A nibble masked out of its word is the fp16 number
+// nibble * 2^-24 (or * 2^-20), subnormal and exact in the matrix instructions: a shift and four masks turn 8 codes into 4
+// operand registers, a packed subtraction takes the 8 out.  The four bits of difference sit in the other operand.
+//   S^T = K q^T: contraction steps of 32 channels, so a group's sum is finished after group / 32 of them and is scaled there.
+//   O^T = V^T P^T: the sums run over keys, whose scales are the weights' business: P is formed once per group of channels as
+//         fp16(exp2(s - M) * scale).  V is transposed by the LDS read that transposes nibbles; the keys of an operand are in
+//         the order in which the score tiles leave them, so P never leaves its registers.
+//
+// The reference M bounds what is rounded to fp16: it is raised where some exp2(s - M) * scale passes 2^12 (or the weights
+// of 32 keys 2^45), to the largest s + log2(scale) less 4.  So the fp16 range is spent on what reaches the output, whatever the scales
+// are: a key with large values and next to no weight leaves the others their precision.  The sums l and O are fp32.
 #include "sage_serving.h"
 #include "sage_device.h"
 
 namespace sage {
 
+typedef float c4f __attribute__((ext_vector_type(4)));
+typedef unsigned c4u __attribute__((ext_vector_type(4)));
+typedef unsigned c2u __attribute__((ext_vector_type(2)));
+typedef int c2i __attribute__((ext_vector_type(2)));
+
 namespace {
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float UNSET = -1e30f;             // a reference below every score: the first key that is seen raises it
+constexpr float W_LIMIT = 4096.0f, P_LIMIT = 0x1p45f;
+constexpr float RAISE = 4.0f, SMALLEST = 0x1p-36f;
+constexpr int TILE = 64, WAVES = 4;
 
-__device__ __forceinline__ float element(const void* p, long at, int type) {
-    if (type == TYPE_F16) return (float)((const _Float16*)p)[at];
-    return __builtin_bit_cast(float, (unsigned)((const unsigned short*)p)[at] << 16);
+// 8 codes of a word -> operand registers: element 2 m + s is nibble m + 4 s, as a multiple of 2^-24 (m even) or 2^-20 (m odd)
+__device__ __forceinline__ half8 operand(unsigned w) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    const unsigned x = w >> 8;
+    const h2 even = __builtin_bit_cast(h2, 0x00080008u), odd = __builtin_bit_cast(h2, 0x00800080u);
+    const h2 a = __builtin_bit_cast(h2, w & 0x000f000fu) - even, b = __builtin_bit_cast(h2, w & 0x00f000f0u) - odd;
+    const h2 c = __builtin_bit_cast(h2, x & 0x000f000fu) - even, d = __builtin_bit_cast(h2, x & 0x00f000f0u) - odd;
+    return (half8){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-// channel d of token `row` of a block
-__device__ __forceinline__ float key_value(const Cache4& c, const unsigned char* block, int row, int d) {
-    const int word = (d & 31) / 8 * (c.D / 32) + d / 32, e = d & 7;
-    const unsigned w = ((const unsigned*)(block + c.k_codes(row)))[word];
-    return (float)((int)(w >> (4 * (e >> 1) + 16 * (e & 1)) & 15u) - 8) * (float)((const _Float16*)(block + c.k_scales(row)))[d / c.group];
-}
-__device__ __forceinline__ float value_value(const Cache4& c, const unsigned char* block, int row, int d) {
-    const unsigned w = ((const unsigned*)(block + c.v_codes(row)))[d / 8];
-    return (float)((int)(w >> 4 * (d & 7) & 15u) - 8) * (float)((const _Float16*)(block + c.v_scales(row)))[d / c.group];
-}
-__device__ __forceinline__ float wg_reduce(float x, bool sum, float* red) {
-    for (int off = 32; off; off >>= 1) {
-        const float y = __shfl_xor(x, off, 64);
-        x = sum ? x + y : __builtin_fmaxf(x, y);
+
+// What a row of queries sees.
+struct RowRange {
+    int length, count;          // of the sequence, limited to what there is
+    int rows;                   // rows that are there: count * share
+    __device__ __forceinline__ RowRange(const Cache4& c, const CacheQueries& q, int b, int share) {
+        length = min(max(q.lengths[b], 0), c.capacity());
+        count = q.count != nullptr ? min(max(q.count[b], 0), q.Nq) : q.Nq;
+        rows = count * share;
     }
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
-    __syncthreads();
-    return sum ? red[0] + red[1] + red[2] + red[3] : __builtin_fmaxf(__builtin_fmaxf(red[0], red[1]), __builtin_fmaxf(red[2], red[3]));
+    // slots [0, end) for query t
+    __device__ __forceinline__ int end(int t, int causal) const { return causal ? max(min(length, length - count + t + 1), 0) : length; }
+};
+
+// 16 rows of queries as the second operand of the score product: lane (column lane % 16, h = lane / 16) holds channels 32 i + 8 h
+// .. of row `row` (the caller's, one that is there).  A row is brought to a largest magnitude of 2^14 .. 2^15 by a power of two,
+// exact for fp16 and for the part of bf16 that matters beside the row's largest, and the elements that meet nibbles of
+// weight 2^-20 are 2^-4 of that.  -> what turns a scaled sum into the exponent of 2.
+template <int D>
+struct Queries4 {
+    half8 op[D / 32];
+    __device__ __forceinline__ float load(const CacheQueries& q, long at, int h) {
+        float x[D / 32][8], m = 0.0f;
+        if (q.type == TYPE_F16) {
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                const half8 v = *(const half8*)((const _Float16*)q.q + at + 32 * i + 8 * h);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[i][e] = (float)v[e];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                const c4u v = *(const c4u*)((const unsigned short*)q.q + at + 32 * i + 8 * h);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const unsigned w = v[e];
+                    x[i][2 * e] = word_f32(w << 16);
+                    x[i][2 * e + 1] = word_f32(w & 0xffff0000u);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = __builtin_fmaxf(m, __builtin_fabsf(x[i][e]));
+        m = __builtin_fmaxf(m, __shfl_xor(m, 16, 64));
+        m = __builtin_fmaxf(m, __shfl_xor(m, 32, 64));
+        const int exponent = __builtin_amdgcn_frexp_expf(m);        // (0 of 0 and of infinity)
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) op[i][e] = (_Float16)ldexpf(x[i][e], 15 - exponent - (e & 2 ? 4 : 0));
+        return __builtin_fmaxf(ldexpf(q.sm_scale * LOG2E, 24 - 15 + exponent), 1e-37f);
+    }
+};
+
+// Where the 16-key pieces of a tile of 64 keys lie: uniform over the wavefront.  A piece without a page (or past the table)
+// points at block 0, which is read and masked.
+struct Pieces {
+    const unsigned char* at[4];
+    int row[4];
+    unsigned bad;
+    __device__ __forceinline__ void find(const Cache4& c, const int* table, int head, int k0) {
+        bad = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int k = k0 + 16 * j, col = k >> c.shift;
+            const int p = col < c.columns ? __builtin_amdgcn_readfirstlane(table[col]) : -1;
+            const bool ok = (unsigned)p < (unsigned)c.num_pages;
+            at[j] = c.data + ((size_t)(ok ? p : 0) * c.heads + head) * c.block_bytes();
+            row[j] = k & (c.page() - 1);
+            if (!ok) bad |= 1u << j;
+        }
+    }
+};
+
+template <int NG> struct ScaleWord;
+template <> struct ScaleWord<4> { typedef c2u type; };
+template <> struct ScaleWord<2> { typedef unsigned type; };
+template <> struct ScaleWord<1> { typedef unsigned short type; };
+
+// A tile of 64 keys on its way: K's words as operands want them, V's rows, a key's scales per lane.
+template <int D, int NG, bool VALUES>
+struct KeyTile {
+    typedef typename ScaleWord<NG>::type scale_t;
+    typedef unsigned words __attribute__((ext_vector_type(D / 32)));
+    words k[4];
+    c4u v[D / 32];
+    scale_t ks, vs;
+    unsigned bad;
+    __device__ __forceinline__ void request(const Cache4& c, const Pieces& p, int lane) {
+        constexpr int ROW = D / 2;
+        const int col = lane & 15, h = lane >> 4;
+        bad = p.bad;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k[j] = *(const words*)(p.at[j] + (p.row[j] + col) * ROW + h * (D / 8));
+        const unsigned char* mine = p.at[0];
+        int r = p.row[0];
+#pragma unroll
+        for (int j = 1; j < 4; ++j) {
+            mine = h == j ? p.at[j] : mine;
+            r = h == j ? p.row[j] : r;
+        }
+        r += col;
+        ks = *(const scale_t*)(mine + (D << c.shift) + r * 2 * NG);
+        if (VALUES) {
+            vs = *(const scale_t*)(mine + ((D + 2 * NG) << c.shift) + r * 2 * NG);
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                // 1 KB at a time: 16 rows of 64 bytes, or 32 of 32
+                if constexpr (D == 128) v[i] = *(const c4u*)(p.at[i] + (ROW << c.shift) + p.row[i] * ROW + lane * 16);
+                else {
+                    const unsigned char* half = lane < 32 ? p.at[2 * i] : p.at[2 * i + 1];
+                    v[i] = *(const c4u*)(half + (ROW << c.shift) + (lane < 32 ? p.row[2 * i] : p.row[2 * i + 1]) * ROW + (lane & 31) * 16);
+                }
+            }
+        }
+    }
+};
+
+// the LDS of a wavefront: V's rows in 16-byte chunks, exchanged so that the 16 rows a transposing read takes lie in different
+// banks; a key's scales
+template <int D, int NG>
+struct WaveLds {
+    unsigned char v[TILE * D / 2];
+    _Float16 ks[TILE * NG], vs[TILE * NG];
+};
+template <int D> __device__ __forceinline__ int v_chunk(int key, int chunk) {
+    return key * (D / 2) + ((chunk ^ (((key >> 4) + (key >> 2)) & (D / 32 - 1))) * 16);
+}
+
+// scores of 16 keys and 16 rows, scaled by K's scales: register r is key 4 h + r
+template <int D, int NG>
+__device__ __forceinline__ c4f scores(const half8 (&k)[D / 32], const half8 (&q)[D / 32], const _Float16 (&ks)[4 * NG]) {
+    constexpr int STEPS = D / 32 / NG;
+    c4f s;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        c4f a = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) a = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[g * STEPS + i], q[g * STEPS + i], a, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[r] = __builtin_fmaf((float)ks[r * NG + g], a[r], g == 0 ? 0.0f : s[r]);
+    }
+    return s;
+}
+
+__device__ __forceinline__ void wave_order() {       // LDS written by other lanes of the wavefront: in program order
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+__device__ __forceinline__ float over_h(float x, bool sum) {
+    const float y = __shfl_xor(x, 16, 64);
+    x = sum ? x + y : __builtin_fmaxf(x, y);
+    const float z = __shfl_xor(x, 32, 64);
+    return sum ? x + z : __builtin_fmaxf(x, z);
 }
 }  // namespace
 
-// The simple form: a workgroup per query row, 256 keys at a time.
-__global__ void __launch_bounds__(256) cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides os, float* __restrict__ lse) {
-    __shared__ float s_q[128], s_p[256], red[4];
-    const int t = threadIdx.x;
-    const int n = blockIdx.x % q.Nq, hq = blockIdx.x / q.Nq % q.Hq, b = blockIdx.x / (q.Nq * q.Hq), h = hq / (q.Hq / c.heads);
-    const int length = min(max(q.lengths[b], 0), c.capacity()), count = q.count != nullptr ? min(max(q.count[b], 0), q.Nq) : q.Nq;
-    const int end = n >= count ? 0 : (q.causal ? min(length, length - count + n + 1) : length);
-    if (t < c.D) s_q[t] = element(q.q, b * q.strides.b + hq * q.strides.h + n * q.strides.n + t, q.type) * q.sm_scale;
-    __syncthreads();
-    float top = -__builtin_inff(), sum = 0.0f, acc = 0.0f;
-    for (int j0 = 0; j0 < end; j0 += 256) {
-        const int j = j0 + t;
-        const unsigned char* block = j < end ? c.block(b, h, j) : nullptr;
-        float s = -__builtin_inff();
-        if (block != nullptr) {
-            s = 0.0f;
-            for (int d = 0; d < c.D; ++d) s = __builtin_fmaf(s_q[d], key_value(c, block, j & (c.page() - 1), d), s);
+// grid: (tile of rows, chunk of keys, (sequence, head)) from one index.  part != nullptr: partial results, [chunk][slab][row][D]
+// normalized fp32 and the base-2 logarithm of their sums.
+template <int D, int NG, int QT>
+__global__ void __launch_bounds__(WAVES * 64, QT == 1 ? 2 : 1)
+cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides os, float* __restrict__ lse, float* __restrict__ part,
+                   float* __restrict__ part_lse, int tiles, int n_splits, int chunk) {
+    constexpr int CT = D / 16;
+    typedef WaveLds<D, NG> Lds;
+    constexpr int MERGE = WAVES * CT * 64 * 16, STAGE = WAVES * (int)sizeof(Lds);
+    __shared__ __attribute__((aligned(16))) unsigned char lds[MERGE > STAGE ? MERGE : STAGE];
+    __shared__ float s_m[WAVES][16], s_l[WAVES][16];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
+    const int slabs = q.B * c.heads, per_slab = tiles * n_splits;
+    // slabs dealt out to the XCDs, so that the workgroups of one share its keys in one L2
+    int slab, rest;
+    if (slabs % 8 == 0) {
+        const int i = blockIdx.x >> 3;
+        slab = (i / per_slab) * 8 + (blockIdx.x & 7);
+        rest = i % per_slab;
+    } else {
+        slab = blockIdx.x / per_slab;
+        rest = blockIdx.x % per_slab;
+    }
+    const int split = rest % n_splits, tile = tiles - 1 - rest / n_splits;
+    const int b = slab / c.heads, head = slab - b * c.heads, share = q.Hq / c.heads;
+    const RowRange range(c, q, b, share);
+    const int row0 = tile * 16 * QT, all_rows = q.Nq * share;
+    const int there = min(range.rows - row0, 16 * QT);               // rows of this workgroup that are there
+    const int first_end = there > 0 ? range.end(row0 / share, q.causal) : 0;
+    const int last_end = there > 0 ? range.end((row0 + there - 1) / share, q.causal) : 0;
+    const int k_begin = split * chunk, k_end = min(k_begin + chunk, last_end);
+    if (part != nullptr && k_begin >= last_end) return;              // (the merge knows)
+
+    Queries4<D> query[QT];
+    float sc[QT], M[QT], l[QT];
+    int end[QT];
+    c4f o[QT][CT];
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        const int row = row0 + min(16 * i + col, max(there - 1, 0)), tq = row / share, g = row - tq * share;
+        sc[i] = query[i].load(q, b * q.strides.b + (head * share + g) * q.strides.h + tq * q.strides.n, h);
+        end[i] = range.end(tq, q.causal);
+        M[i] = UNSET;
+        l[i] = 0.0f;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) o[i][ct] = (c4f){0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    Lds& mine = *(Lds*)(lds + wave * sizeof(Lds));
+    const int* const table = c.table + (size_t)b * c.columns;
+    KeyTile<D, NG, true> next;
+    int k0 = k_begin + TILE * wave;
+    Pieces pieces;
+    if (k0 < k_end) {
+        pieces.find(c, table, head, k0);
+        next.request(c, pieces, lane);
+    }
+    for (; k0 < k_end; k0 += TILE * WAVES) {
+        KeyTile<D, NG, true> now = next;
+        wave_order();
+        // ---- V and the scales to LDS.  A row past the last key holds anything, its scale is no number perhaps: 0 instead.
+        const bool absent = k0 + lane >= last_end || (now.bad >> h & 1);
+        *(typename ScaleWord<NG>::type*)(mine.ks + lane * NG) = absent ? (typename ScaleWord<NG>::type)(0) : now.ks;
+        *(typename ScaleWord<NG>::type*)(mine.vs + lane * NG) = absent ? (typename ScaleWord<NG>::type)(0) : now.vs;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            const int key = (i * 1024 + lane * 16) / (D / 2), ch = lane % (D / 32);
+            *(c4u*)(mine.v + v_chunk<D>(key, ch)) = now.v[i];
         }
-        const float most = __builtin_fmaxf(top, wg_reduce(s, false, red));
-        const float sub = most == -__builtin_inff() ? 0.0f : most;
-        const float p = expf(s - sub), keep = expf(top - sub);
-        top = most;
-        sum = sum * keep + wg_reduce(p, true, red);
-        acc *= keep;
-        s_p[t] = p;
-        __syncthreads();
-        if (t < c.D)
-            for (int i = 0; i < min(256, end - j0); ++i) {
-                const unsigned char* at = c.block(b, h, j0 + i);
-                if (at != nullptr) acc = __builtin_fmaf(s_p[i], value_value(c, at, (j0 + i) & (c.page() - 1), t), acc);
+        wave_order();
+        if (k0 + TILE * WAVES < k_end) {
+            pieces.find(c, table, head, k0 + TILE * WAVES);
+            next.request(c, pieces, lane);
+        }
+        // ---- V transposed: lane's channel 16 ct + lane % 16, nibble i of its words: key 16 (i / 4) + 4 h + i % 4
+        c2i vt[CT];
+        const int v_key = 16 * (col >> 2) + 4 * h + (col & 3);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+            vt[ct] = __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) c2i*)(mine.v + v_chunk<D>(v_key, ct >> 1) + 8 * (ct & 1)));
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            // ---- 32 keys: pieces 2 u and 2 u + 1
+            half8 k[2][D / 32];
+            _Float16 ks[2][4 * NG], vs[2][4 * NG];
+            typedef _Float16 scales_t __attribute__((ext_vector_type(4 * NG)));
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) k[j][i] = operand(now.k[2 * u + j][i]);
+                const scales_t a = *(const scales_t*)(mine.ks + (16 * (2 * u + j) + 4 * h) * NG);
+                const scales_t d = *(const scales_t*)(mine.vs + (16 * (2 * u + j) + 4 * h) * NG);
+#pragma unroll
+                for (int e = 0; e < 4 * NG; ++e) {
+                    ks[j][e] = a[e];
+                    vs[j][e] = d[e];
+                }
             }
-        __syncthreads();
-    }
-    const float r = sum == 0.0f ? 0.0f : acc / sum;
-    if (t < c.D) {
-        const long at = b * os.b + hq * os.h + n * os.n + t;
-        if (q.type == TYPE_F16) ((_Float16*)out)[at] = (_Float16)r;
-        else ((__bf16*)out)[at] = (__bf16)r;
-    }
-    if (t == 0 && lse != nullptr) lse[((long)b * q.Hq + hq) * q.Nq + n] = sum == 0.0f ? -__builtin_inff() : top + logf(sum);
-}
-
-// A thread per key.
-__global__ void __launch_bounds__(256) cache4_weights_kernel(Cache4 c, CacheQueries q, const float* __restrict__ lse, const float* __restrict__ weights,
-                                                             float* __restrict__ out, int width) {
-    const int bh = blockIdx.y, b = bh / c.heads, h = bh - b * c.heads, j = blockIdx.x * 256 + threadIdx.x;
-    if (j >= width) return;
-    const int length = min(max(q.lengths[b], 0), c.capacity()), count = q.count != nullptr ? min(max(q.count[b], 0), q.Nq) : q.Nq;
-    const unsigned char* block = j < length ? c.block(b, h, j) : nullptr;
-    const int share = q.Hq / c.heads;
-    float sum = 0.0f;
-    for (int g = 0; g < share; ++g)
-        for (int n = 0; n < count; ++n) {
-            if (block == nullptr || (q.causal && j > length - count + n)) continue;
-            const long at = b * q.strides.b + (h * share + g) * q.strides.h + n * q.strides.n;
-            float s = 0.0f;
-            for (int d = 0; d < c.D; ++d) s = __builtin_fmaf(element(q.q, at + d, q.type), key_value(c, block, j & (c.page() - 1), d), s);
-            const float l = lse[((long)b * q.Hq + h * share + g) * q.Nq + n];
-            if (l != -__builtin_inff()) sum += expf(s * q.sm_scale - l);
+            half8 v[CT];
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) v[ct] = operand((unsigned)vt[ct][u]);
+            const bool masked = k0 + 32 * u + 32 > first_end || (now.bad >> 2 * u & 3) != 0;
+#pragma unroll
+            for (int i = 0; i < QT; ++i) {
+                float s[2][4];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const c4f a = scores<D, NG>(k[j], query[i].op, ks[j]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[j][r] = a[r];
+                }
+                if (masked) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int last = now.bad >> (2 * u + j) & 1 ? 0 : end[i];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (k0 + 16 * (2 * u + j) + 4 * h + r >= last) s[j][r] = -__builtin_inff();
+                    }
+                }
+                half8 w[NG];
+                float sum;
+                auto weigh = [&]() {
+                    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+                    h2 top = {0, 0};
+                    sum = 0.0f;
+                    const float M_odd = M[i] + 4.0f;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float p[2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][r], sc[i], r & 1 ? -M_odd : -M[i]));
+                            sum = r & 1 ? __builtin_fmaf(p[j], 16.0f, sum) : sum + p[j];
+                        }
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) {
+                            const h2 x = {(_Float16)__builtin_fmaf(p[0], (float)vs[0][r * NG + g], 0.0f),
+                                          (_Float16)__builtin_fmaf(p[1], (float)vs[1][r * NG + g], 0.0f)};
+                            w[g][2 * r] = x[0];
+                            w[g][2 * r + 1] = x[1];
+                            top = __builtin_elementwise_max(top, x);
+                        }
+                    }
+                    return __builtin_amdgcn_ballot_w64(sum > P_LIMIT || (float)__builtin_fmaxf16(top[0], top[1]) > W_LIMIT) != 0ull;
+                };
+                if (__builtin_expect(weigh(), 0)) {
+                    float most = -__builtin_inff();
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            float scale = SMALLEST;
+#pragma unroll
+                            for (int g = 0; g < NG; ++g) scale = __builtin_fmaxf(scale, (float)vs[j][r * NG + g]);
+                            most = __builtin_fmaxf(most, __builtin_fmaf(s[j][r], sc[i], __builtin_amdgcn_logf(scale) - RAISE));
+                        }
+                    const float M_new = __builtin_fmaxf(M[i], over_h(most, false));
+                    const float alpha = __builtin_amdgcn_exp2f(M[i] - M_new);
+                    M[i] = M_new;
+                    l[i] *= alpha;
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[i][ct][r] *= alpha;
+                    weigh();
+                }
+                l[i] += sum;
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+                    o[i][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[ct], w[ct * NG / CT], o[i][ct], 0, 0, 0);
+            }
         }
-    const size_t at = (size_t)bh * width + j;
-    out[at] = (weights != nullptr ? weights[at] : 0.0f) + sum;
+    }
+
+    // ---- the wavefronts' results: O = sum f_w O_w / sum f_w l_w, f_w = 2^(M_w - max M)
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        const float lw = over_h(l[i], true);
+        __syncthreads();                // the tiles, or the query tile before, have been read
+        if (h == 0) {
+            s_m[wave][col] = M[i];
+            s_l[wave][col] = lw;
+        }
+        __syncthreads();
+        float top = s_m[0][col], total = 0.0f;
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) top = __builtin_fmaxf(top, s_m[w][col]);
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) total = __builtin_fmaf(s_l[w][col], __builtin_amdgcn_exp2f(s_m[w][col] - top), total);
+        const float f = __builtin_amdgcn_exp2f(M[i] - top);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) *(c4f*)(lds + ((wave * CT + ct) * 64 + lane) * 16) = o[i][ct] * f;
+        __syncthreads();
+        const int row = row0 + 16 * i + col;
+        if (row >= all_rows) continue;
+        const bool live = row < range.rows;
+        const float norm = live && total != 0.0f ? 0x1p24f / total : 0.0f;
+        const float log_sum = live && total != 0.0f ? top + __builtin_amdgcn_logf(total) : -__builtin_inff();
+        const int tq = row / share, g = row - tq * share;
+        const size_t prow = ((size_t)split * slabs + slab) * all_rows + row;
+        if (wave == 0 && h == 0) {
+            if (part != nullptr) part_lse[prow] = log_sum;
+            else if (lse != nullptr) lse[((size_t)b * q.Hq + head * share + g) * q.Nq + tq] = log_sum * LN2;
+        }
+#pragma unroll
+        for (int n = 0; n < CT / WAVES; ++n) {
+            const int ct = wave + WAVES * n;
+            c4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) x += *(const c4f*)(lds + ((w * CT + ct) * 64 + lane) * 16);
+            x = norm == 0.0f ? (c4f){0.0f, 0.0f, 0.0f, 0.0f} : x * norm;
+            const int d = 16 * ct + 4 * h;
+            if (part != nullptr) {
+                *(c4f*)(part + prow * D + d) = x;
+            } else {
+                const long at = b * os.b + (head * share + g) * os.h + tq * os.n + d;
+                if (q.type == TYPE_F16) {
+                    typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+                    *(h4*)((_Float16*)out + at) = __builtin_convertvector(x, h4);
+                } else {
+                    typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+                    *(b4*)((__bf16*)out + at) = __builtin_convertvector(x, b4);
+                }
+            }
+        }
+    }
 }
 
-size_t cache4_attn_workspace(int B, int Hq, int Hkv, int Nq, int D, int capacity, int n_splits) { return 0; }
+// O = sum_s w_s O_s / sum_s w_s, w_s = 2^(lse_s - max lse): D / 4 threads per row, 4 channels each.
+template <int D>
+__global__ void __launch_bounds__(256) cache4_merge_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides os, float* __restrict__ lse,
+                                                           const float* __restrict__ part, const float* __restrict__ part_lse, int chunk) {
+    constexpr int TPR = D / 4, ROWS = 256 / TPR;
+    const int share = q.Hq / c.heads, all_rows = q.Nq * share, slabs = q.B * c.heads;
+    const long at_row = (long)blockIdx.x * ROWS + threadIdx.x / TPR;
+    if (at_row >= (long)slabs * all_rows) return;
+    const int slab = (int)(at_row / all_rows), row = (int)(at_row - (long)slab * all_rows), d = threadIdx.x % TPR * 4;
+    const int b = slab / c.heads, head = slab - b * c.heads, tq = row / share, g = row - tq * share;
+    const RowRange range(c, q, b, share);
+    const int end = row < range.rows ? range.end(tq, q.causal) : 0, n = (end + chunk - 1) / chunk;
+    const long step = (long)slabs * all_rows;
+    float top = -__builtin_inff(), total = 0.0f;
+    for (int s = 0; s < n; ++s) top = __builtin_fmaxf(top, part_lse[s * step + at_row]);
+    c4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (top > -__builtin_inff())
+        for (int s = 0; s < n; ++s) {
+            const float w = __builtin_amdgcn_exp2f(part_lse[s * step + at_row] - top);
+            total += w;
+            x += *(const c4f*)(part + (s * step + at_row) * D + d) * w;
+        }
+    if (total != 0.0f) x *= 1.0f / total;
+    if (d == 0 && lse != nullptr)
+        lse[((size_t)b * q.Hq + head * share + g) * q.Nq + tq] = total != 0.0f ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
+    const long at = b * os.b + (head * share + g) * os.h + tq * os.n + d;
+    if (q.type == TYPE_F16) {
+        typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+        *(h4*)((_Float16*)out + at) = __builtin_convertvector(x, h4);
+    } else {
+        typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+        *(b4*)((__bf16*)out + at) = __builtin_convertvector(x, b4);
+    }
+}
+
+// A workgroup takes 256 keys of a (sequence, head), a wavefront 64 of them, whose operands stay in its registers while it walks
+// the rows 16 at a time; a lane's sums belong to 16 keys and one column of rows, and the columns are added at the end.
+template <int D, int NG>
+__global__ void __launch_bounds__(WAVES * 64) cache4_weights_kernel(Cache4 c, CacheQueries q, const float* __restrict__ lse,
+                                                                    const float* __restrict__ weights, float* __restrict__ out, int width) {
+    __shared__ __attribute__((aligned(16))) _Float16 s_ks[WAVES][TILE * NG];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
+    const int slab = blockIdx.y, b = slab / c.heads, head = slab - b * c.heads, share = q.Hq / c.heads;
+    const int k0 = (blockIdx.x * WAVES + wave) * TILE;
+    if (k0 >= width) return;
+    const RowRange range(c, q, b, share);
+    float sum[4][4] = {};
+    const int last_end = range.rows > 0 ? range.end(range.count - 1, q.causal) : 0;
+    if (k0 < last_end) {
+        Pieces pieces;
+        pieces.find(c, c.table + (size_t)b * c.columns, head, k0);
+        KeyTile<D, NG, false> tile;
+        tile.request(c, pieces, lane);
+        *(typename ScaleWord<NG>::type*)(s_ks[wave] + lane * NG) = tile.ks;
+        wave_order();
+        half8 k[4][D / 32];
+        _Float16 ks[4][4 * NG];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            typedef _Float16 scales_t __attribute__((ext_vector_type(4 * NG)));
+            const scales_t a = *(const scales_t*)(s_ks[wave] + (16 * j + 4 * h) * NG);
+#pragma unroll
+            for (int e = 0; e < 4 * NG; ++e) ks[j][e] = a[e];
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) k[j][i] = operand(tile.k[j][i]);
+        }
+        for (int row0 = 0; row0 < range.rows; row0 += 16) {
+            const int row = min(row0 + col, range.rows - 1), tq = row / share, g = row - tq * share;
+            const int end = row0 + col < range.rows ? range.end(tq, q.causal) : 0;
+            if (range.end(min(row0 + 15, range.rows - 1) / share, q.causal) <= k0) continue;
+            Queries4<D> query;
+            const float sc = query.load(q, b * q.strides.b + (head * share + g) * q.strides.h + tq * q.strides.n, h);
+            float L = lse[((size_t)b * q.Hq + head * share + g) * q.Nq + tq] * LOG2E;
+            if (L == -__builtin_inff()) L = __builtin_inff();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const c4f s = scores<D, NG>(k[j], query.op, ks[j]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, -L));
+                    sum[j][r] += k0 + 16 * j + 4 * h + r < end ? p : 0.0f;
+                }
+            }
+        }
+        // the 16 columns of rows
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float x = sum[j][r];
+#pragma unroll
+                for (int off = 8; off; off >>= 1) x += __shfl_xor(x, off, 64);
+                sum[j][r] = tile.bad >> j & 1 ? 0.0f : x;
+            }
+    }
+    // lane (col, h) writes key 16 (col / 4) + 4 h + col % 4
+    float mine = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mine = col == 4 * j + r ? sum[j][r] : mine;
+    const int key = k0 + 16 * (col >> 2) + 4 * h + (col & 3);
+    if (key < width) {
+        const size_t at = (size_t)slab * width + key;
+        out[at] = (weights != nullptr ? weights[at] : 0.0f) + mine;
+    }
+}
+
+namespace {
+// How a call is cut.  Rows: 16, 32 or 64 per workgroup, so that a cache is read once for as many as there are.  Keys: chunks of a
+// multiple of 256, as many as it takes to have WANTED workgroups, none shorter than 512 unless the caller asks for it.
+struct AttnPlan {
+    int qt, tiles, n_splits, chunk;
+};
+constexpr int WANTED = 1024;
+AttnPlan plan(int B, int Hq, int Hkv, int Nq, int capacity, int requested) {
+    const int rows = Hq / Hkv * Nq;
+    AttnPlan p;
+    p.qt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    p.tiles = (rows + 16 * p.qt - 1) / (16 * p.qt);
+    const long groups = (long)B * Hkv * p.tiles;
+    long n = requested > 0 ? requested : WANTED / groups;
+    const int least = requested > 0 ? 256 : 512;
+    if (n > capacity / least) n = capacity / least;
+    if (n < 1) n = 1;
+    p.chunk = (int)(((capacity + n - 1) / n + 255) / 256 * 256);
+    p.n_splits = (capacity + p.chunk - 1) / p.chunk;
+    return p;
+}
+}  // namespace
+
+size_t cache4_attn_workspace(int B, int Hq, int Hkv, int Nq, int D, int capacity, int n_splits) {
+    const AttnPlan p = plan(B, Hq, Hkv, Nq, capacity, n_splits);
+    return p.n_splits <= 1 ? 0 : (size_t)p.n_splits * B * Hq * Nq * (D + 1) * sizeof(float);
+}
+
+template <int D, int NG>
+static void launch_attn_form(const AttnPlan& p, const Cache4& c, const CacheQueries& q, void* out, const RowStrides& os, float* lse, float* part,
+                             float* part_lse, hipStream_t st) {
+    const unsigned grid = (unsigned)(q.B * c.heads * p.tiles * p.n_splits);
+#define SAGE_CACHE4_ATTN(QT) cache4_attn_kernel<D, NG, QT><<<grid, WAVES * 64, 0, st>>>(c, q, out, os, lse, part, part_lse, p.tiles, p.n_splits, p.chunk)
+    if (p.qt == 1) SAGE_CACHE4_ATTN(1);
+    else if (p.qt == 2) SAGE_CACHE4_ATTN(2);
+    else SAGE_CACHE4_ATTN(4);
+#undef SAGE_CACHE4_ATTN
+}
 
 hipError_t launch_cache4_attn(const Cache4& c, const CacheQueries& q, void* out, const RowStrides& os, float* lse, void* workspace,
                               int n_splits, hipStream_t st) {
-    cache4_attn_kernel<<<q.B * q.Hq * q.Nq, 256, 0, st>>>(c, q, out, os, lse);
+    const AttnPlan p = plan(q.B, q.Hq, c.heads, q.Nq, c.capacity(), n_splits);
+    const size_t rows = (size_t)q.B * q.Hq * q.Nq;
+    float* const part = p.n_splits > 1 ? (float*)workspace : nullptr;
+    float* const part_lse = p.n_splits > 1 ? part + p.n_splits * rows * c.D : nullptr;
+    const int ng = c.scales();
+    if (c.D == 64) {
+        if (ng == 1) launch_attn_form<64, 1>(p, c, q, out, os, lse, part, part_lse, st);
+        else launch_attn_form<64, 2>(p, c, q, out, os, lse, part, part_lse, st);
+    } else {
+        if (ng == 1) launch_attn_form<128, 1>(p, c, q, out, os, lse, part, part_lse, st);
+        else if (ng == 2) launch_attn_form<128, 2>(p, c, q, out, os, lse, part, part_lse, st);
+        else launch_attn_form<128, 4>(p, c, q, out, os, lse, part, part_lse, st);
+    }
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || p.n_splits <= 1) return e;
+    const unsigned per = 256 / (c.D / 4), grid = (unsigned)((rows + per - 1) / per);
+    if (c.D == 64) cache4_merge_kernel<64><<<grid, 256, 0, st>>>(c, q, out, os, lse, part, part_lse, p.chunk);
+    else cache4_merge_kernel<128><<<grid, 256, 0, st>>>(c, q, out, os, lse, part, part_lse, p.chunk);
     return hipGetLastError();
 }
 
 hipError_t launch_cache4_weights(const Cache4& c, const CacheQueries& q, const float* lse, const float* weights, float* out, int width,
                                  hipStream_t st) {
-    cache4_weights_kernel<<<dim3((width + 255) / 256, q.B * c.heads), 256, 0, st>>>(c, q, lse, weights, out, width);
+    const dim3 grid((width + WAVES * TILE - 1) / (WAVES * TILE), q.B * c.heads);
+    const int ng = c.scales();
+#define SAGE_CACHE4_WEIGHTS(D, NG) cache4_weights_kernel<D, NG><<<grid, WAVES * 64, 0, st>>>(c, q, lse, weights, out, width)
+    if (c.D == 64 && ng == 1) SAGE_CACHE4_WEIGHTS(64, 1);
+    else if (c.D == 64) SAGE_CACHE4_WEIGHTS(64, 2);
+    else if (ng == 1) SAGE_CACHE4_WEIGHTS(128, 1);
+    else if (ng == 2) SAGE_CACHE4_WEIGHTS(128, 2);
+    else SAGE_CACHE4_WEIGHTS(128, 4);
+#undef SAGE_CACHE4_WEIGHTS
     return hipGetLastError();
 }
 
