@@ -9,9 +9,8 @@
 // of one (sequence, key head) and its four wavefronts take tiles of 64 keys in turn, each with its own running reference, sum
 // and O, without a barrier, and add up at the end; long caches are cut into chunks for several workgroups and merged.
 //
-// Codes go to the matrix pipe as they are, scales are applied to sums.  A nibble masked out of its word is the fp16 number
-// nibble * 2^-24 (or * 2^-20), subnormal and exact in the matrix instructions: a shift and four masks turn 8 codes into 4
-// operand registers, a packed subtraction takes the 8 out.  The four bits of difference sit in the other operand.
+// Codes go to the matrix pipe as whole numbers, scales are applied to sums: 9 vector instructions turn 8 codes into 4 operand
+// registers (operand()), every other pair 16 times too large, for which the other operand makes up.
 //   S^T = K q^T: contraction steps of 32 channels, so a group's sum is finished after group / 32 of them and is scaled there.
 //   O^T = V^T P^T: the sums run over keys, whose scales are the weights' business: P is formed once per group of channels as
 //         fp16(exp2(s - M) * scale).  V is transposed by the LDS read that transposes nibbles; the keys of an operand are in
@@ -33,17 +32,27 @@ typedef int c2i __attribute__((ext_vector_type(2)));
 namespace {
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float UNSET = -1e30f;             // a reference below every score: the first key that is seen raises it
-constexpr float W_LIMIT = 4096.0f, P_LIMIT = 0x1p45f;
+constexpr _Float16 W_LIMIT = 4096.0f;
+constexpr float P_LIMIT = 0x1p45f;
 constexpr float RAISE = 4.0f, SMALLEST = 0x1p-36f;
 constexpr int TILE = 64, WAVES = 4;
 
-// 8 codes of a word -> operand registers: element 2 m + s is nibble m + 4 s, as a multiple of 2^-24 (m even) or 2^-20 (m odd)
+// 8 codes of a word -> operand registers: element 2 m + s is the code of nibble m + 4 s, times 16 where m is odd.  A nibble in the
+// low mantissa bits of 1024 is 1024 + nibble (or + 16 nibble); the packed subtraction is exact and leaves a small whole number.
+// (The nibbles as subnormal numbers would need no exponent and, with the 8 in the other terms, no subtraction: 9 -> 5
+// instructions.  But the matrix pipe aligns a subnormal operand's products as if it were 2^-14, which costs the sums 7 bits.)
+// (Written as one instruction because the compiler takes two for constants that are both scalar.)
+__device__ __forceinline__ unsigned and_or(unsigned w, unsigned mask, unsigned bits) {
+    unsigned d;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(d) : "v"(w), "s"(mask), "v"(bits));
+    return d;
+}
 __device__ __forceinline__ half8 operand(unsigned w) {
     typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-    const unsigned x = w >> 8;
-    const h2 even = __builtin_bit_cast(h2, 0x00080008u), odd = __builtin_bit_cast(h2, 0x00800080u);
-    const h2 a = __builtin_bit_cast(h2, w & 0x000f000fu) - even, b = __builtin_bit_cast(h2, w & 0x00f000f0u) - odd;
-    const h2 c = __builtin_bit_cast(h2, x & 0x000f000fu) - even, d = __builtin_bit_cast(h2, x & 0x00f000f0u) - odd;
+    const unsigned x = w >> 8, thousand = 0x64006400u;
+    const h2 even = {(_Float16)1032.0f, (_Float16)1032.0f}, odd = {(_Float16)1152.0f, (_Float16)1152.0f};
+    const h2 a = __builtin_bit_cast(h2, and_or(w, 0x000f000fu, thousand)) - even, b = __builtin_bit_cast(h2, and_or(w, 0x00f000f0u, thousand)) - odd;
+    const h2 c = __builtin_bit_cast(h2, and_or(x, 0x000f000fu, thousand)) - even, d = __builtin_bit_cast(h2, and_or(x, 0x00f000f0u, thousand)) - odd;
     return (half8){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
@@ -61,9 +70,9 @@ struct RowRange {
 };
 
 // 16 rows of queries as the second operand of the score product: lane (column lane % 16, h = lane / 16) holds channels 32 i + 8 h
-// .. of row `row` (the caller's, one that is there).  A row is brought to a largest magnitude of 2^14 .. 2^15 by a power of two,
-// exact for fp16 and for the part of bf16 that matters beside the row's largest, and the elements that meet nibbles of
-// weight 2^-20 are 2^-4 of that.  -> what turns a scaled sum into the exponent of 2.
+// .. of the row at `at`.  A row is brought to a largest magnitude of 2^13 .. 2^14 by a power of two, so that every element that
+// matters beside the largest is exact in fp16, bf16's range and the 2^-4 of those that meet 16-fold codes included.
+// -> what turns a scaled sum into the exponent of 2.
 template <int D>
 struct Queries4 {
     half8 op[D / 32];
@@ -98,27 +107,24 @@ struct Queries4 {
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) op[i][e] = (_Float16)ldexpf(x[i][e], 15 - exponent - (e & 2 ? 4 : 0));
-        return __builtin_fmaxf(ldexpf(q.sm_scale * LOG2E, 24 - 15 + exponent), 1e-37f);
+            for (int e = 0; e < 8; ++e) op[i][e] = (_Float16)ldexpf(x[i][e], 14 - exponent - (e & 2 ? 4 : 0));
+        return __builtin_fmaxf(ldexpf(q.sm_scale * LOG2E, exponent - 14), 1e-37f);
     }
 };
 
-// Where the 16-key pieces of a tile of 64 keys lie: uniform over the wavefront.  A piece without a page (or past the table)
-// points at block 0, which is read and masked.
-struct Pieces {
-    const unsigned char* at[4];
-    int row[4];
-    unsigned bad;
-    __device__ __forceinline__ void find(const Cache4& c, const int* table, int head, int k0) {
-        bad = 0;
+// The pages of a tile's four 16-key pieces (of the whole tile where a page holds 64 tokens or more: id[0]), uniform over the
+// wavefront; looked up a tile before they are used.  -1: none.
+struct PageIds {
+    int id[4];
+    __device__ __forceinline__ void look_up(const Cache4& c, const int* table, int k0) {
+        const int n = c.shift >= 6 ? 1 : 4;
+        const int col = k0 >> c.shift;
+        id[0] = col < c.columns ? table[col] : -1;
+        if (n == 1) return;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int k = k0 + 16 * j, col = k >> c.shift;
-            const int p = col < c.columns ? __builtin_amdgcn_readfirstlane(table[col]) : -1;
-            const bool ok = (unsigned)p < (unsigned)c.num_pages;
-            at[j] = c.data + ((size_t)(ok ? p : 0) * c.heads + head) * c.block_bytes();
-            row[j] = k & (c.page() - 1);
-            if (!ok) bad |= 1u << j;
+        for (int j = 1; j < 4; ++j) {
+            const int cj = (k0 + 16 * j) >> c.shift;
+            id[j] = cj < c.columns ? table[cj] : -1;
         }
     }
 };
@@ -128,59 +134,100 @@ template <> struct ScaleWord<4> { typedef c2u type; };
 template <> struct ScaleWord<2> { typedef unsigned type; };
 template <> struct ScaleWord<1> { typedef unsigned short type; };
 
-// A tile of 64 keys on its way: K's words as operands want them, V's rows, a key's scales per lane.
+// A tile of 64 keys on its way: K's words as operands want them, V's rows, a key's scales per lane.  A piece without a page
+// reads block 0 instead, and is masked.
 template <int D, int NG, bool VALUES>
 struct KeyTile {
     typedef typename ScaleWord<NG>::type scale_t;
     typedef unsigned words __attribute__((ext_vector_type(D / 32)));
+    static constexpr int ROW = D / 2;
     words k[4];
-    c4u v[D / 32];
+    c4u v[VALUES ? D / 32 : 1];
     scale_t ks, vs;
-    unsigned bad;
-    __device__ __forceinline__ void request(const Cache4& c, const Pieces& p, int lane) {
-        constexpr int ROW = D / 2;
-        const int col = lane & 15, h = lane >> 4;
-        bad = p.bad;
+    unsigned bad;               // bit j: piece j has no page
+    // head: the block of the key head in page 0
+    static __device__ __forceinline__ const unsigned char* block(const Cache4& c, const unsigned char* head, int id, bool& ok) {
+        ok = (unsigned)id < (unsigned)c.num_pages;
+        return head + (size_t)(unsigned)__builtin_amdgcn_readfirstlane(ok ? id : 0) * (c.heads * c.block_bytes());
+    }
+    __device__ __forceinline__ void request(const Cache4& c, const unsigned char* head, const PageIds& pages, int k0, int lane) {
+        const int col = lane & 15, h = lane >> 4, mask = c.page() - 1;
+        if (c.shift >= 6) {
+            bool ok;
+            const unsigned char* const at = block(c, head, pages.id[0], ok);
+            const int row = k0 & mask;
+            bad = ok ? 0u : 15u;
+            const unsigned char* const kp = at + row * ROW;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) k[j] = *(const words*)(p.at[j] + (p.row[j] + col) * ROW + h * (D / 8));
-        const unsigned char* mine = p.at[0];
-        int r = p.row[0];
+            for (int j = 0; j < 4; ++j) k[j] = *(const words*)(kp + col * ROW + h * (D / 8) + 16 * j * ROW);
+            const unsigned char* const sp = at + (D << c.shift) + row * 2 * NG;
+            ks = *(const scale_t*)(sp + lane * 2 * NG);
+            if constexpr (VALUES) {
+                vs = *(const scale_t*)(sp + (2 * NG << c.shift) + lane * 2 * NG);
+                const unsigned char* const vp = kp + (ROW << c.shift);
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) v[i] = *(const c4u*)(vp + lane * 16 + 1024 * i);
+            }
+            return;
+        }
+        const unsigned char* at[4];
+        int row[4];
+        bad = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            bool ok;
+            at[j] = block(c, head, pages.id[j], ok);
+            row[j] = (k0 + 16 * j) & mask;
+            if (!ok) bad |= 1u << j;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k[j] = *(const words*)(at[j] + (row[j] + col) * ROW + h * (D / 8));
+        const unsigned char* mine = at[0];
+        int r = row[0];
 #pragma unroll
         for (int j = 1; j < 4; ++j) {
-            mine = h == j ? p.at[j] : mine;
-            r = h == j ? p.row[j] : r;
+            mine = h == j ? at[j] : mine;
+            r = h == j ? row[j] : r;
         }
         r += col;
         ks = *(const scale_t*)(mine + (D << c.shift) + r * 2 * NG);
-        if (VALUES) {
+        if constexpr (VALUES) {
             vs = *(const scale_t*)(mine + ((D + 2 * NG) << c.shift) + r * 2 * NG);
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) {
                 // 1 KB at a time: 16 rows of 64 bytes, or 32 of 32
-                if constexpr (D == 128) v[i] = *(const c4u*)(p.at[i] + (ROW << c.shift) + p.row[i] * ROW + lane * 16);
+                if constexpr (D == 128) v[i] = *(const c4u*)(at[i] + (ROW << c.shift) + row[i] * ROW + lane * 16);
                 else {
-                    const unsigned char* half = lane < 32 ? p.at[2 * i] : p.at[2 * i + 1];
-                    v[i] = *(const c4u*)(half + (ROW << c.shift) + (lane < 32 ? p.row[2 * i] : p.row[2 * i + 1]) * ROW + (lane & 31) * 16);
+                    const unsigned char* half = lane < 32 ? at[2 * i] : at[2 * i + 1];
+                    v[i] = *(const c4u*)(half + (ROW << c.shift) + (lane < 32 ? row[2 * i] : row[2 * i + 1]) * ROW + (lane & 31) * 16);
                 }
             }
         }
     }
 };
 
-// the LDS of a wavefront: V's rows in 16-byte chunks, exchanged so that the 16 rows a transposing read takes lie in different
-// banks; a key's scales
+// The LDS of a wavefront: K's words, each lane's own (so that the registers are free for the next tile at once); V's rows in
+// 16-byte chunks, exchanged so that the 16 rows a transposing read takes lie in different banks; a key's scales.
 template <int D, int NG>
 struct WaveLds {
-    unsigned char v[TILE * D / 2];
+    unsigned char k[TILE * D / 2], v[TILE * D / 2];
     _Float16 ks[TILE * NG], vs[TILE * NG];
 };
 template <int D> __device__ __forceinline__ int v_chunk(int key, int chunk) {
     return key * (D / 2) + ((chunk ^ (((key >> 4) + (key >> 2)) & (D / 32 - 1))) * 16);
 }
 
+// the larger of three, of both halves (a NaN stays)
+__device__ __forceinline__ unsigned max3_pairs(unsigned a, unsigned b, unsigned c) {
+    unsigned d;
+    asm("v_pk_maximum3_f16 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+    return d;
+}
+__device__ __forceinline__ _Float16 half_of(unsigned w, int hi) { return __builtin_bit_cast(_Float16, (unsigned short)(hi ? w >> 16 : w)); }
+
 // scores of 16 keys and 16 rows, scaled by K's scales: register r is key 4 h + r
 template <int D, int NG>
-__device__ __forceinline__ c4f scores(const half8 (&k)[D / 32], const half8 (&q)[D / 32], const _Float16 (&ks)[4 * NG]) {
+__device__ __forceinline__ c4f scores(const half8 (&k)[D / 32], const half8 (&q)[D / 32], const unsigned (&ks)[2 * NG]) {
     constexpr int STEPS = D / 32 / NG;
     c4f s;
 #pragma unroll
@@ -189,9 +236,68 @@ __device__ __forceinline__ c4f scores(const half8 (&k)[D / 32], const half8 (&q)
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) a = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[g * STEPS + i], q[g * STEPS + i], a, 0, 0, 0);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s[r] = __builtin_fmaf((float)ks[r * NG + g], a[r], g == 0 ? 0.0f : s[r]);
+        for (int r = 0; r < 4; ++r) s[r] = __builtin_fmaf((float)half_of(ks[(r * NG + g) / 2], (r * NG + g) & 1), a[r], g == 0 ? 0.0f : s[r]);
     }
     return s;
+}
+
+// The weights of 32 keys for 16 rows: register r of the two score tiles is keys 4 h + r and 16 + 4 h + r, element 2 r and 2 r + 1
+// of an operand; those of odd r meet 16-fold codes and are 2^-4 of the others.  -> whether the reference is too low.
+template <int NG, class S>
+__device__ __forceinline__ bool weigh(const float (&s)[2][4], float sc, float M, const S (&vs)[2], half8 (&w)[NG], float& sum) {
+    unsigned x[NG][4];
+    const float M_odd = M + 4.0f;
+    sum = 0.0f;
+    auto one = [&](auto R) {
+        constexpr int r = decltype(R)::value;
+        float p[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][r], sc, r & 1 ? -M_odd : -M));
+            sum = r & 1 ? __builtin_fmaf(p[j], 16.0f, sum) : sum + p[j];
+        }
+        auto group = [&](auto G) {
+            constexpr int g = decltype(G)::value, at = r * NG + g;
+            // (two products and a conversion: the instructions that multiply into half a register take twice as long)
+            if constexpr (g < NG) {
+                typedef float f2 __attribute__((ext_vector_type(2)));
+                typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+                const f2 y = {__builtin_fmaf(p[0], (float)half_of(vs[0][at / 2], at & 1), 0.0f), __builtin_fmaf(p[1], (float)half_of(vs[1][at / 2], at & 1), 0.0f)};
+                x[g][r] = __builtin_bit_cast(unsigned, __builtin_convertvector(y, h2));
+            }
+        };
+        group(std::integral_constant<int, 0>{});
+        group(std::integral_constant<int, 1>{});
+        group(std::integral_constant<int, 2>{});
+        group(std::integral_constant<int, 3>{});
+    };
+    one(std::integral_constant<int, 0>{});
+    one(std::integral_constant<int, 1>{});
+    one(std::integral_constant<int, 2>{});
+    one(std::integral_constant<int, 3>{});
+    unsigned top = 0;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        top = max3_pairs(top, x[g][0], x[g][1]);
+        top = max3_pairs(top, x[g][2], x[g][3]);
+        w[g] = __builtin_bit_cast(half8, (c4u){x[g][0], x[g][1], x[g][2], x[g][3]});
+    }
+    return __builtin_amdgcn_ballot_w64(sum > P_LIMIT || half_of(top, 0) > W_LIMIT || half_of(top, 1) > W_LIMIT) != 0ull;
+}
+// the reference that a lane's 8 keys ask for
+template <int NG, class S>
+__device__ __forceinline__ float reference(const float (&s)[2][4], float sc, const S (&vs)[2]) {
+    float most = -__builtin_inff();
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float scale = SMALLEST;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) scale = __builtin_fmaxf(scale, (float)half_of(vs[j][(r * NG + g) / 2], (r * NG + g) & 1));
+            most = __builtin_fmaxf(most, __builtin_fmaf(s[j][r], sc, __builtin_amdgcn_logf(scale) - RAISE));
+        }
+    return most;
 }
 
 __device__ __forceinline__ void wave_order() {       // LDS written by other lanes of the wavefront: in program order
@@ -209,10 +315,10 @@ __device__ __forceinline__ float over_h(float x, bool sum) {
 // grid: (tile of rows, chunk of keys, (sequence, head)) from one index.  part != nullptr: partial results, [chunk][slab][row][D]
 // normalized fp32 and the base-2 logarithm of their sums.
 template <int D, int NG, int QT>
-__global__ void __launch_bounds__(WAVES * 64, QT == 1 ? 2 : 1)
+__global__ void __launch_bounds__(WAVES * 64, QT == 1 ? 3 : 2)
 cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides os, float* __restrict__ lse, float* __restrict__ part,
                    float* __restrict__ part_lse, int tiles, int n_splits, int chunk) {
-    constexpr int CT = D / 16;
+    constexpr int CT = D / 16, STEPS = D / 32 / NG;
     typedef WaveLds<D, NG> Lds;
     constexpr int MERGE = WAVES * CT * 64 * 16, STAGE = WAVES * (int)sizeof(Lds);
     __shared__ __attribute__((aligned(16))) unsigned char lds[MERGE > STAGE ? MERGE : STAGE];
@@ -229,10 +335,10 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
         slab = blockIdx.x / per_slab;
         rest = blockIdx.x % per_slab;
     }
-    const int split = rest % n_splits, tile = tiles - 1 - rest / n_splits;
+    const int split = rest % n_splits;
     const int b = slab / c.heads, head = slab - b * c.heads, share = q.Hq / c.heads;
     const RowRange range(c, q, b, share);
-    const int row0 = tile * 16 * QT, all_rows = q.Nq * share;
+    const int row0 = (tiles - 1 - rest / n_splits) * 16 * QT, all_rows = q.Nq * share;
     const int there = min(range.rows - row0, 16 * QT);               // rows of this workgroup that are there
     const int first_end = there > 0 ? range.end(row0 / share, q.causal) : 0;
     const int last_end = there > 0 ? range.end((row0 + there - 1) / share, q.causal) : 0;
@@ -256,127 +362,99 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
 
     Lds& mine = *(Lds*)(lds + wave * sizeof(Lds));
     const int* const table = c.table + (size_t)b * c.columns;
-    KeyTile<D, NG, true> next;
+    const unsigned char* const head_at = c.data + head * c.block_bytes();
+    typedef KeyTile<D, NG, true> Tile;
+    typedef typename Tile::words words;
+    constexpr int NEXT = TILE * WAVES;
+    Tile tile;
+    PageIds pages;
     int k0 = k_begin + TILE * wave;
-    Pieces pieces;
     if (k0 < k_end) {
-        pieces.find(c, table, head, k0);
-        next.request(c, pieces, lane);
+        pages.look_up(c, table, k0);
+        tile.request(c, head_at, pages, k0, lane);
+        pages.look_up(c, table, k0 + NEXT);
     }
-    for (; k0 < k_end; k0 += TILE * WAVES) {
-        KeyTile<D, NG, true> now = next;
+    for (; k0 < k_end; k0 += NEXT) {
         wave_order();
-        // ---- V and the scales to LDS.  A row past the last key holds anything, its scale is no number perhaps: 0 instead.
-        const bool absent = k0 + lane >= last_end || (now.bad >> h & 1);
-        *(typename ScaleWord<NG>::type*)(mine.ks + lane * NG) = absent ? (typename ScaleWord<NG>::type)(0) : now.ks;
-        *(typename ScaleWord<NG>::type*)(mine.vs + lane * NG) = absent ? (typename ScaleWord<NG>::type)(0) : now.vs;
+        // ---- the tile to LDS.  The scales of a row past the last key are perhaps no numbers: 0 instead.
+        const unsigned bad = tile.bad;
+        const bool absent = k0 + lane >= last_end || (bad >> h & 1);
+        *(typename Tile::scale_t*)(mine.ks + lane * NG) = absent ? (typename Tile::scale_t)(0) : tile.ks;
+        *(typename Tile::scale_t*)(mine.vs + lane * NG) = absent ? (typename Tile::scale_t)(0) : tile.vs;
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-            const int key = (i * 1024 + lane * 16) / (D / 2), ch = lane % (D / 32);
-            *(c4u*)(mine.v + v_chunk<D>(key, ch)) = now.v[i];
-        }
+        for (int i = 0; i < D / 32; ++i) *(c4u*)(mine.v + v_chunk<D>((i * 1024 + lane * 16) / (D / 2), lane % (D / 32))) = tile.v[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ((words*)mine.k)[j * 64 + lane] = tile.k[j];
         wave_order();
-        if (k0 + TILE * WAVES < k_end) {
-            pieces.find(c, table, head, k0 + TILE * WAVES);
-            next.request(c, pieces, lane);
+        if (k0 + NEXT < k_end) {
+            tile.request(c, head_at, pages, k0 + NEXT, lane);
+            pages.look_up(c, table, k0 + 2 * NEXT);
         }
-        // ---- V transposed: lane's channel 16 ct + lane % 16, nibble i of its words: key 16 (i / 4) + 4 h + i % 4
-        c2i vt[CT];
         const int v_key = 16 * (col >> 2) + 4 * h + (col & 3);
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-            vt[ct] = __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) c2i*)(mine.v + v_chunk<D>(v_key, ct >> 1) + 8 * (ct & 1)));
-#pragma unroll
         for (int u = 0; u < 2; ++u) {
-            // ---- 32 keys: pieces 2 u and 2 u + 1
-            half8 k[2][D / 32];
-            _Float16 ks[2][4 * NG], vs[2][4 * NG];
-            typedef _Float16 scales_t __attribute__((ext_vector_type(4 * NG)));
+            // ---- 32 keys: pieces 2 u and 2 u + 1.  An operand is made when its products are due and feeds all tiles of rows.
+            typedef unsigned scales_t __attribute__((ext_vector_type(2 * NG)));
+            scales_t vs[2];
+            float s[QT][2][4];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
+                const words kw = ((const words*)mine.k)[(2 * u + j) * 64 + lane];
+                const scales_t ks = *(const scales_t*)(mine.ks + (16 * (2 * u + j) + 4 * h) * NG);
+                vs[j] = *(const scales_t*)(mine.vs + (16 * (2 * u + j) + 4 * h) * NG);
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) k[j][i] = operand(now.k[2 * u + j][i]);
-                const scales_t a = *(const scales_t*)(mine.ks + (16 * (2 * u + j) + 4 * h) * NG);
-                const scales_t d = *(const scales_t*)(mine.vs + (16 * (2 * u + j) + 4 * h) * NG);
+                for (int g = 0; g < NG; ++g) {
+                    c4f a[QT];
 #pragma unroll
-                for (int e = 0; e < 4 * NG; ++e) {
-                    ks[j][e] = a[e];
-                    vs[j][e] = d[e];
-                }
-            }
-            half8 v[CT];
+                    for (int n = 0; n < STEPS; ++n) {
+                        const half8 k = operand(kw[g * STEPS + n]);
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) v[ct] = operand((unsigned)vt[ct][u]);
-            const bool masked = k0 + 32 * u + 32 > first_end || (now.bad >> 2 * u & 3) != 0;
-#pragma unroll
-            for (int i = 0; i < QT; ++i) {
-                float s[2][4];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const c4f a = scores<D, NG>(k[j], query[i].op, ks[j]);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) s[j][r] = a[r];
-                }
-                if (masked) {
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int last = now.bad >> (2 * u + j) & 1 ? 0 : end[i];
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (k0 + 16 * (2 * u + j) + 4 * h + r >= last) s[j][r] = -__builtin_inff();
+                        for (int i = 0; i < QT; ++i)
+                            a[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, query[i].op[g * STEPS + n], n == 0 ? (c4f){0.0f, 0.0f, 0.0f, 0.0f} : a[i], 0, 0, 0);
                     }
-                }
-                half8 w[NG];
-                float sum;
-                auto weigh = [&]() {
-                    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-                    h2 top = {0, 0};
-                    sum = 0.0f;
-                    const float M_odd = M[i] + 4.0f;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        float p[2];
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][r], sc[i], r & 1 ? -M_odd : -M[i]));
-                            sum = r & 1 ? __builtin_fmaf(p[j], 16.0f, sum) : sum + p[j];
-                        }
-#pragma unroll
-                        for (int g = 0; g < NG; ++g) {
-                            const h2 x = {(_Float16)__builtin_fmaf(p[0], (float)vs[0][r * NG + g], 0.0f),
-                                          (_Float16)__builtin_fmaf(p[1], (float)vs[1][r * NG + g], 0.0f)};
-                            w[g][2 * r] = x[0];
-                            w[g][2 * r + 1] = x[1];
-                            top = __builtin_elementwise_max(top, x);
-                        }
-                    }
-                    return __builtin_amdgcn_ballot_w64(sum > P_LIMIT || (float)__builtin_fmaxf16(top[0], top[1]) > W_LIMIT) != 0ull;
-                };
-                if (__builtin_expect(weigh(), 0)) {
-                    float most = -__builtin_inff();
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
+                    for (int i = 0; i < QT; ++i)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            float scale = SMALLEST;
-#pragma unroll
-                            for (int g = 0; g < NG; ++g) scale = __builtin_fmaxf(scale, (float)vs[j][r * NG + g]);
-                            most = __builtin_fmaxf(most, __builtin_fmaf(s[j][r], sc[i], __builtin_amdgcn_logf(scale) - RAISE));
+                            const float scale = (float)half_of(ks[(r * NG + g) / 2], (r * NG + g) & 1);
+                            s[i][j][r] = __builtin_fmaf(scale, a[i][r], g == 0 ? 0.0f : s[i][j][r]);
                         }
-                    const float M_new = __builtin_fmaxf(M[i], over_h(most, false));
+                }
+            }
+            if (k0 + 32 * u + 32 > first_end || (bad >> 2 * u & 3) != 0) {
+#pragma unroll
+                for (int i = 0; i < QT; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int last = bad >> (2 * u + j) & 1 ? 0 : end[i];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (k0 + 16 * (2 * u + j) + 4 * h + r >= last) s[i][j][r] = -__builtin_inff();
+                    }
+            }
+            half8 w[QT][NG];
+#pragma unroll
+            for (int i = 0; i < QT; ++i) {
+                float sum;
+                if (__builtin_expect(weigh<NG>(s[i], sc[i], M[i], vs, w[i], sum), 0)) {
+                    const float M_new = __builtin_fmaxf(M[i], over_h(reference<NG>(s[i], sc[i], vs), false));
                     const float alpha = __builtin_amdgcn_exp2f(M[i] - M_new);
                     M[i] = M_new;
                     l[i] *= alpha;
 #pragma unroll
-                    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) o[i][ct][r] *= alpha;
-                    weigh();
+                    for (int ct = 0; ct < CT; ++ct) o[i][ct] *= alpha;
+                    weigh<NG>(s[i], sc[i], M[i], vs, w[i], sum);
                 }
                 l[i] += sum;
+            }
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-                    o[i][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[ct], w[ct * NG / CT], o[i][ct], 0, 0, 0);
+            for (int ct = 0; ct < CT; ++ct) {
+                // V transposed: channel 16 ct + lane % 16, nibble i of the words: key 16 (i / 4) + 4 h + i % 4
+                const c2i vt = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
+                    (__attribute__((address_space(3))) c2i*)(mine.v + v_chunk<D>(v_key, ct >> 1) + 8 * (ct & 1)));
+                const half8 v = operand((unsigned)vt[u]);
+#pragma unroll
+                for (int i = 0; i < QT; ++i) o[i][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[i][ct * NG / CT], o[i][ct], 0, 0, 0);
             }
         }
     }
@@ -403,7 +481,7 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
         const int row = row0 + 16 * i + col;
         if (row >= all_rows) continue;
         const bool live = row < range.rows;
-        const float norm = live && total != 0.0f ? 0x1p24f / total : 0.0f;
+        const float norm = live && total != 0.0f ? 1.0f / total : 0.0f;
         const float log_sum = live && total != 0.0f ? top + __builtin_amdgcn_logf(total) : -__builtin_inff();
         const int tq = row / share, g = row - tq * share;
         const size_t prow = ((size_t)split * slabs + slab) * all_rows + row;
@@ -435,28 +513,73 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
     }
 }
 
-// O = sum_s w_s O_s / sum_s w_s, w_s = 2^(lse_s - max lse): D / 4 threads per row, 4 channels each.
-template <int D>
+// O = sum_s w_s O_s / sum_s w_s, w_s = 2^(lse_s - max lse).  D / 4 threads hold a row, 4 channels each; LANES such groups take
+// every LANES-th chunk, BATCH of them requested before the first is used, and add up through LDS.  Few rows of many chunks
+// (a decoding step) have the whole workgroup on a row, many rows one group each.
+template <int D, int LANES, int BATCH>
 __global__ void __launch_bounds__(256) cache4_merge_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides os, float* __restrict__ lse,
                                                            const float* __restrict__ part, const float* __restrict__ part_lse, int chunk) {
-    constexpr int TPR = D / 4, ROWS = 256 / TPR;
+    constexpr int TPR = D / 4, ROWS = 256 / (TPR * LANES);
+    __shared__ c4f s_x[LANES > 1 ? 256 : 1];
+    __shared__ float s_top[LANES > 1 ? LANES : 1], s_sum[LANES > 1 ? LANES : 1];
     const int share = q.Hq / c.heads, all_rows = q.Nq * share, slabs = q.B * c.heads;
-    const long at_row = (long)blockIdx.x * ROWS + threadIdx.x / TPR;
-    if (at_row >= (long)slabs * all_rows) return;
+    const long at_row = (long)blockIdx.x * ROWS + (LANES > 1 ? 0 : threadIdx.x / TPR);
+    if (at_row >= (long)slabs * all_rows) return;                    // (with several groups on a row: all of them)
     const int slab = (int)(at_row / all_rows), row = (int)(at_row - (long)slab * all_rows), d = threadIdx.x % TPR * 4;
     const int b = slab / c.heads, head = slab - b * c.heads, tq = row / share, g = row - tq * share;
     const RowRange range(c, q, b, share);
     const int end = row < range.rows ? range.end(tq, q.causal) : 0, n = (end + chunk - 1) / chunk;
+    const int first = LANES > 1 ? threadIdx.x / TPR : 0;
     const long step = (long)slabs * all_rows;
-    float top = -__builtin_inff(), total = 0.0f;
-    for (int s = 0; s < n; ++s) top = __builtin_fmaxf(top, part_lse[s * step + at_row]);
+    float top = UNSET, total = 0.0f;
     c4f x = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (top > -__builtin_inff())
-        for (int s = 0; s < n; ++s) {
-            const float w = __builtin_amdgcn_exp2f(part_lse[s * step + at_row] - top);
-            total += w;
-            x += *(const c4f*)(part + (s * step + at_row) * D + d) * w;
+    for (int s0 = first; s0 < n; s0 += LANES * BATCH) {
+        float ls[BATCH];
+        c4f y[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            // (past the last chunk: the last one again, with weight 0)
+            const int s = s0 + i * LANES, sc = s < n ? s : n - 1;
+            const float v = part_lse[sc * step + at_row];
+            y[i] = *(const c4f*)(part + (sc * step + at_row) * D + d);
+            ls[i] = s < n ? v : -__builtin_inff();
         }
+        __builtin_amdgcn_sched_barrier(0);
+        float most = top;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) most = __builtin_fmaxf(most, ls[i]);
+        const float keep = __builtin_amdgcn_exp2f(top - most);
+        top = most;
+        total *= keep;
+        x *= keep;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const float w = __builtin_amdgcn_exp2f(ls[i] - top);
+            total += w;
+            x += y[i] * w;
+        }
+    }
+    if constexpr (LANES > 1) {
+        s_x[threadIdx.x] = x;
+        if (threadIdx.x % TPR == 0) {
+            s_top[first] = top;
+            s_sum[first] = total;
+        }
+        __syncthreads();
+        if (first != 0) return;
+        float most = s_top[0];
+#pragma unroll
+        for (int i = 1; i < LANES; ++i) most = __builtin_fmaxf(most, s_top[i]);
+        total = 0.0f;
+        x = (c4f){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < LANES; ++i) {
+            const float f = __builtin_amdgcn_exp2f(s_top[i] - most);
+            total = __builtin_fmaf(s_sum[i], f, total);
+            x += s_x[i * TPR + threadIdx.x] * f;
+        }
+        top = most;
+    }
     if (total != 0.0f) x *= 1.0f / total;
     if (d == 0 && lse != nullptr)
         lse[((size_t)b * q.Hq + head * share + g) * q.Nq + tq] = total != 0.0f ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
@@ -484,20 +607,20 @@ __global__ void __launch_bounds__(WAVES * 64) cache4_weights_kernel(Cache4 c, Ca
     float sum[4][4] = {};
     const int last_end = range.rows > 0 ? range.end(range.count - 1, q.causal) : 0;
     if (k0 < last_end) {
-        Pieces pieces;
-        pieces.find(c, c.table + (size_t)b * c.columns, head, k0);
+        PageIds pages;
+        pages.look_up(c, c.table + (size_t)b * c.columns, k0);
         KeyTile<D, NG, false> tile;
-        tile.request(c, pieces, lane);
+        tile.request(c, c.data + head * c.block_bytes(), pages, k0, lane);
         *(typename ScaleWord<NG>::type*)(s_ks[wave] + lane * NG) = tile.ks;
         wave_order();
         half8 k[4][D / 32];
-        _Float16 ks[4][4 * NG];
+        unsigned ks[4][2 * NG];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            typedef _Float16 scales_t __attribute__((ext_vector_type(4 * NG)));
+            typedef unsigned scales_t __attribute__((ext_vector_type(2 * NG)));
             const scales_t a = *(const scales_t*)(s_ks[wave] + (16 * j + 4 * h) * NG);
 #pragma unroll
-            for (int e = 0; e < 4 * NG; ++e) ks[j][e] = a[e];
+            for (int e = 0; e < 2 * NG; ++e) ks[j][e] = a[e];
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) k[j][i] = operand(tile.k[j][i]);
         }
@@ -544,16 +667,18 @@ __global__ void __launch_bounds__(WAVES * 64) cache4_weights_kernel(Cache4 c, Ca
 }
 
 namespace {
-// How a call is cut.  Rows: 16, 32 or 64 per workgroup, so that a cache is read once for as many as there are.  Keys: chunks of a
-// multiple of 256, as many as it takes to have WANTED workgroups, none shorter than 512 unless the caller asks for it.
+// How a call is cut.  Rows: 16 or 32 per workgroup.  (64, with one wavefront per SIMD: 64 rows of 64 slabs of 16K keys 95 us, two
+// workgroups of 32 rows 90; 4096 rows of 8 slabs of 8K 233 / 216.)  Keys: chunks of a multiple of 256, as many as it takes to have
+// WANTED workgroups, two per compute unit (us with 256 / 512 / 1024 workgroups: 256 slabs of 16K keys 146 / 112 / 110, 8 of 128K 40 / 36 /
+// 40, 64 of 16K with 64 rows 110 / 90 / 98), none shorter than 512 unless the caller asks for it.
 struct AttnPlan {
     int qt, tiles, n_splits, chunk;
 };
-constexpr int WANTED = 1024;
+constexpr int WANTED = 512;
 AttnPlan plan(int B, int Hq, int Hkv, int Nq, int capacity, int requested) {
     const int rows = Hq / Hkv * Nq;
     AttnPlan p;
-    p.qt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    p.qt = rows <= 16 ? 1 : 2;
     p.tiles = (rows + 16 * p.qt - 1) / (16 * p.qt);
     const long groups = (long)B * Hkv * p.tiles;
     long n = requested > 0 ? requested : WANTED / groups;
@@ -577,8 +702,7 @@ static void launch_attn_form(const AttnPlan& p, const Cache4& c, const CacheQuer
     const unsigned grid = (unsigned)(q.B * c.heads * p.tiles * p.n_splits);
 #define SAGE_CACHE4_ATTN(QT) cache4_attn_kernel<D, NG, QT><<<grid, WAVES * 64, 0, st>>>(c, q, out, os, lse, part, part_lse, p.tiles, p.n_splits, p.chunk)
     if (p.qt == 1) SAGE_CACHE4_ATTN(1);
-    else if (p.qt == 2) SAGE_CACHE4_ATTN(2);
-    else SAGE_CACHE4_ATTN(4);
+    else SAGE_CACHE4_ATTN(2);
 #undef SAGE_CACHE4_ATTN
 }
 
@@ -598,9 +722,11 @@ hipError_t launch_cache4_attn(const Cache4& c, const CacheQueries& q, void* out,
         else launch_attn_form<128, 4>(p, c, q, out, os, lse, part, part_lse, st);
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess || p.n_splits <= 1) return e;
-    const unsigned per = 256 / (c.D / 4), grid = (unsigned)((rows + per - 1) / per);
-    if (c.D == 64) cache4_merge_kernel<64><<<grid, 256, 0, st>>>(c, q, out, os, lse, part, part_lse, p.chunk);
-    else cache4_merge_kernel<128><<<grid, 256, 0, st>>>(c, q, out, os, lse, part, part_lse, p.chunk);
+#define SAGE_CACHE4_MERGE(D, LANES, BATCH) cache4_merge_kernel<D, LANES, BATCH><<<(unsigned)((rows * (D / 4) * LANES + 255) / 256), 256, 0, st>>>(c, q, out, os, lse, part, part_lse, p.chunk)
+    const bool wide = rows <= 2048 && p.n_splits > 4;
+    if (c.D == 64) { if (wide) SAGE_CACHE4_MERGE(64, 16, 4); else SAGE_CACHE4_MERGE(64, 1, 4); }
+    else { if (wide) SAGE_CACHE4_MERGE(128, 8, 4); else SAGE_CACHE4_MERGE(128, 1, 4); }
+#undef SAGE_CACHE4_MERGE
     return hipGetLastError();
 }
 
