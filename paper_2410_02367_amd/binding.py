@@ -21,7 +21,8 @@ _NATIVE_CALLS = ("sage_quant_q", "sage_rope_quant_q", "sage_smooth_quant_k_works
                  "sage_rope_smooth_quant_k", "sage_quant_qk", "sage_quant_v_workspace", "sage_quant_v",
                  "sage_attn_split_workspace", "sage_attn_cross_fwd", "sage_attn_cross_split_fwd",
                  "sage_attn_pv_int8_cross_fwd", "sage_attn_pv_int8_cross_split_fwd", "sage_attention_workspace",
-                 "sage_attention_fwd")
+                 "sage_attention_fwd", "sage_rope", "sage_rope_bwd", "sage_cache4_block_bytes", "sage_cache4_append", "sage_cache4_load",
+                 "sage_cache4_attn_workspace", "sage_cache4_attn", "sage_cache4_weights", "sage_cache4_evict")
 
 EXPORTS = ("sage_status_string", "sage_source_hash", "sage_default_sm_scale", "sage_quant_q", "sage_smooth_quant_k_workspace",
            "sage_smooth_quant_k", "sage_quant_qk", "sage_smooth_quant_k_noalloc", "sage_rope_quant_q", "sage_rope_smooth_quant_k",

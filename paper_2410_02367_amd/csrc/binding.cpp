@@ -10,7 +10,9 @@
 #include <Python.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <ATen/ops/empty_like.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <cmath>
 #include <cstring>
 
 #include "../../include/sage.h"
@@ -39,6 +41,15 @@ struct Api {
     decltype(&sage_attn_pv_int8_cross_split_fwd) pv8_split;
     decltype(&sage_attention_workspace) attention_workspace;
     decltype(&sage_attention_fwd) attention;
+    decltype(&sage_rope) rope;
+    decltype(&sage_rope_bwd) rope_bwd;
+    decltype(&sage_cache4_block_bytes) cache4_block_bytes;
+    decltype(&sage_cache4_append) cache4_append;
+    decltype(&sage_cache4_load) cache4_load;
+    decltype(&sage_cache4_attn_workspace) cache4_attn_workspace;
+    decltype(&sage_cache4_attn) cache4_attn;
+    decltype(&sage_cache4_weights) cache4_weights;
+    decltype(&sage_cache4_evict) cache4_evict;
 } api;
 PyObject *get_device, *get_stream;          // torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
@@ -332,7 +343,276 @@ PyObject* py_attention(PyObject* const* argv, Py_ssize_t n) {
     return result(call([&] { return api.attention(pq, pk, pv, po, pw, wb, B, H, Nq, Nkv, D, causal != 0, sm, bq, bk, pv8 != 0, st); }), {&o});
 }
 
-// (torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, 15 addresses in Api's order)
+// ---- the serving calls (serving.py): tensors on the current device; the rows of [B, H, N, D] ones lie anywhere
+constexpr auto BF16 = at::kBFloat16, I32 = at::kInt, F64 = at::kDouble;
+
+struct ServingArgs : Args {
+    int device = -1;
+    explicit ServingArgs(PyObject* const* args) : Args(args) {
+        PyObject* d = PyObject_CallNoArgs(get_device);
+        device = d ? (int)PyLong_AsLong(d) : -1;
+        Py_XDECREF(d);
+        if (PyErr_Occurred()) { PyErr_Clear(); ok = false; }
+    }
+    bool here(const at::Tensor& t) const { return t.is_cuda() && t.get_device() == device; }
+    // [B, H, N, D] with neighbouring channels, of a type of these calls
+    const at::Tensor* rows(bool fp32 = false) {
+        const at::Tensor* t = tensor(*a++);
+        ok = ok && t && here(*t) && t->dim() == 4 && (t->scalar_type() == F16 || t->scalar_type() == BF16 || (fp32 && t->scalar_type() == F32)) &&
+             (t->stride(3) == 1 || t->size(3) == 1) && fits(*t);
+        return ok ? t : nullptr;
+    }
+    const at::Tensor* rows_or_none(bool fp32 = false) { return *a == Py_None ? (++a, nullptr) : rows(fp32); }
+    // contiguous, of this type and these sizes (-1: any); null where None is allowed and given
+    const at::Tensor* flat(at::ScalarType type, std::initializer_list<int64_t> sizes, bool optional = false) {
+        PyObject* o = *a++;
+        if (optional && o == Py_None) return nullptr;
+        const at::Tensor* t = tensor(o);
+        ok = ok && t && here(*t) && t->scalar_type() == type && t->dim() == (int64_t)sizes.size() && t->is_contiguous();
+        if (!ok) return nullptr;
+        int i = 0;
+        for (int64_t n : sizes) {
+            const int64_t m = t->size(i++);
+            ok = ok && (n < 0 || n == m) && m <= 0x7fffffff;
+        }
+        return ok ? t : nullptr;
+    }
+    float real_or(float otherwise) {
+        if (*a == Py_None) return ++a, otherwise;
+        return real();
+    }
+};
+struct RowsOf {                 // pointer and strides of a rows() tensor, as the library takes them
+    void* p = nullptr;
+    int64_t s[3] = {0, 0, 0};
+    const int64_t* strides = nullptr;
+    RowsOf() = default;
+    explicit RowsOf(const at::Tensor* t) {
+        if (!t) return;
+        p = t->data_ptr();
+        if (t->is_contiguous()) return;
+        for (int i = 0; i < 3; ++i) s[i] = t->stride(i);
+        strides = s;
+    }
+};
+const void* at_or_null(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+int type_of(const at::Tensor& t) { return t.scalar_type() == F16 ? SAGE_F16 : t.scalar_type() == BF16 ? SAGE_BF16 : SAGE_F32; }
+// an output: the caller's, or a new tensor laid out as `like` is
+struct LikeBuffer : Buffer {
+    bool take_like(const at::Tensor* given, PyObject* object, const at::Tensor& like) {
+        if (given) {
+            from = object;
+            t = given;
+            return given->scalar_type() == like.scalar_type() && given->sizes() == like.sizes();
+        }
+        own = at::empty_like(like);
+        t = &own;
+        return true;
+    }
+};
+// A pool and the table of its pages: (cache, pages), B sequences, checked against the form
+struct CacheOf {
+    const at::Tensor *cache, *pages;
+    bool read(ServingArgs& a, int64_t B) {
+        cache = a.flat(U8, {-1, -1, -1});
+        pages = a.flat(I32, {B, -1});
+        return a.ok;
+    }
+    int num_pages() const { return (int)cache->size(0); }
+    int heads() const { return (int)cache->size(1); }
+    int sequences() const { return (int)pages->size(0); }
+    int columns() const { return (int)pages->size(1); }
+    bool form(int64_t D, int page, int group) const {
+        const size_t need = D > 0 && D < 4096 ? api.cache4_block_bytes((int)D, page, group) : 0;
+        return need != 0 && cache->size(2) == (int64_t)need;
+    }
+};
+
+// (q, k | None, positions, inv_freq, interleaved, amplitude, q_out | None, k_out | None, stream | None)
+template <bool BWD> PyObject* py_rope(PyObject* const* argv, Py_ssize_t n) {
+    if (n != 9) return none();
+    ServingArgs a(argv);
+    const at::Tensor *q = a.rows(true), *k = a.rows_or_none(true);
+    if (!a.ok) return none();
+    const int64_t B = q->size(0), Hq = q->size(1), N = q->size(2), D = q->size(3), Hk = k ? k->size(1) : 0;
+    if (k && (k->scalar_type() != q->scalar_type() || k->size(0) != B || k->size(2) != N || k->size(3) != D)) return none();
+    const at::Tensor* at_pos = tensor(argv[2]);
+    const bool own_positions = at_pos && at_pos->dim() == 2;
+    const at::Tensor* pos = own_positions ? a.flat(I32, {B, N}) : a.flat(I32, {N});
+    const at::Tensor* freq = a.flat(F64, {-1});
+    const int interleaved = a.integer();
+    const float amplitude = a.real();
+    const at::Tensor *gq = a.rows_or_none(true), *gk = a.rows_or_none(true);
+    void* st = a.stream();
+    if (!a.take(gq && (gk || !k)) || (gk && !k)) return none();
+    LikeBuffer oq, ok;
+    if (!oq.take_like(gq, argv[6], *q) || (k && !ok.take_like(gk, argv[7], *k))) return none();
+    const RowsOf xq(q), yq(oq.t), xk(k), yk(k ? ok.t : nullptr);
+    const int type = type_of(*q), rotated = 2 * (int)freq->size(0);
+    const int32_t* pp = (const int32_t*)pos->data_ptr();
+    const double* pf = (const double*)freq->data_ptr();
+    const int e = call([&] {
+        return (BWD ? api.rope_bwd : api.rope)(xq.p, xq.strides, yq.p, yq.strides, xk.p, xk.strides, yk.p, yk.strides, pp, own_positions ? N : 0, pf,
+                                               amplitude, B, Hq, Hk, N, D, rotated, type, interleaved, st);
+    });
+    return k ? result(e, {&oq, &ok}) : result(e, {&oq});
+}
+
+// (k, v, cache, pages, start, count | None, k_mean | None, page, group, stream | None) -> cache
+PyObject* py_cache4_append(PyObject* const* argv, Py_ssize_t n) {
+    if (n != 10) return none();
+    ServingArgs a(argv);
+    const at::Tensor *k = a.rows(), *v = a.rows();
+    if (!a.ok || k->scalar_type() != v->scalar_type() || k->sizes() != v->sizes()) return none();
+    const int64_t B = k->size(0), H = k->size(1), N = k->size(2), D = k->size(3);
+    CacheOf c;
+    if (!c.read(a, B)) return none();
+    const at::Tensor *start = a.flat(I32, {B}), *count = a.flat(I32, {B}, true), *mean = a.flat(F32, {B, H, D}, true);
+    const int page = a.integer(), group = a.integer();
+    void* st = a.stream();
+    if (!a.take(true) || c.heads() != H || !c.form(D, page, group)) return none();
+    const RowsOf rk(k), rv(v);
+    const int type = type_of(*k);
+    const void *pm = at_or_null(mean), *pt = c.pages->data_ptr(), *ps = start->data_ptr(), *pn = at_or_null(count);
+    void* pc = c.cache->data_ptr();
+    const int e = call([&] {
+        return api.cache4_append(rk.p, rk.strides, rv.p, rv.strides, (const float*)pm, pc, (const int32_t*)pt, (const int32_t*)ps, (const int32_t*)pn, B, H, N, D,
+                                 type, c.num_pages(), c.columns(), page, group, st);
+    });
+    return e != 0 ? PyLong_FromLong(e) : (Py_INCREF(argv[2]), argv[2]);
+}
+
+// (cache, pages, start | None, N, D, count | None, k_mean | None, bf16, page, group, k | None, v | None, stream | None)
+PyObject* py_cache4_load(PyObject* const* argv, Py_ssize_t n) {
+    if (n != 13) return none();
+    ServingArgs a(argv);
+    CacheOf c;
+    if (!c.read(a, -1)) return none();
+    const int64_t B = c.sequences(), H = c.heads();
+    const at::Tensor* start = a.flat(I32, {B}, true);
+    const int N = a.integer(), D = a.integer();
+    const at::Tensor *count = a.flat(I32, {B}, true), *mean = a.flat(F32, {B, H, D}, true);
+    const auto type = a.integer() ? BF16 : F16;
+    const int page = a.integer(), group = a.integer();
+    const at::Tensor *gk = a.flat(type, {B, H, N, D}, true), *gv = a.flat(type, {B, H, N, D}, true);
+    void* st = a.stream();
+    if (!a.take(gk && gv) || N <= 0 || !c.form(D, page, group)) return none();
+    Buffer k, v;
+    k.take(gk ? argv[10] : nullptr, *c.cache, {B, H, N, D}, type);
+    v.take(gv ? argv[11] : nullptr, *c.cache, {B, H, N, D}, type);
+    const void *pc = c.cache->data_ptr(), *pt = c.pages->data_ptr(), *ps = at_or_null(start), *pn = at_or_null(count), *pm = at_or_null(mean);
+    void *pk = k.p(), *pv = v.p();
+    return result(call([&] {
+                      return api.cache4_load(pc, (const int32_t*)pt, (const int32_t*)ps, (const int32_t*)pn, (const float*)pm, pk, pv, B, H, N, D,
+                                             type == BF16 ? SAGE_BF16 : SAGE_F16, c.num_pages(), c.columns(), page, group, st);
+                  }),
+                  {&k, &v});
+}
+
+// (q, cache, pages, lengths, count | None, causal, sm_scale | None, page, group, n_splits, return_lse, out | None, lse | None,
+// workspace | None, stream | None)
+PyObject* py_cache4_attn(PyObject* const* argv, Py_ssize_t n) {
+    if (n != 15) return none();
+    ServingArgs a(argv);
+    const at::Tensor* q = a.rows();
+    if (!a.ok) return none();
+    const int64_t B = q->size(0), Hq = q->size(1), Nq = q->size(2), D = q->size(3);
+    CacheOf c;
+    if (!c.read(a, B)) return none();
+    const at::Tensor *lengths = a.flat(I32, {B}), *count = a.flat(I32, {B}, true);
+    const int causal = a.integer();
+    const bool no_scale = argv[6] == Py_None;
+    const float sm = a.real_or(0.0f);
+    const int page = a.integer(), group = a.integer(), splits = a.integer(), with_lse = a.integer();
+    const at::Tensor *go = a.rows_or_none(), *gl = a.flat(F32, {B, Hq, Nq}, true), *gw = a.flat(U8, {-1}, true);
+    void* st = a.stream();
+    if (!a.take(go && (gl || !with_lse) && gw) || splits < 0 || !c.form(D, page, group)) return none();
+    LikeBuffer o;
+    if (!o.take_like(go, argv[11], *q)) return none();
+    Buffer lse, ws;
+    if (gl || with_lse) lse.take(gl ? argv[12] : nullptr, *q, {B, Hq, Nq}, F32);
+    ws.bytes(gw ? argv[13] : nullptr, *q, api.cache4_attn_workspace(B, Hq, c.heads(), Nq, D, c.columns(), page, splits));
+    const RowsOf rq(q), ro(o.t);
+    const int type = type_of(*q);
+    const float scale = no_scale ? 1.0f / std::sqrt((float)D) : sm;
+    const void *pc = c.cache->data_ptr(), *pt = c.pages->data_ptr(), *pl = lengths->data_ptr(), *pn = at_or_null(count);
+    void *ps = lse.p(), *pw = ws.p();
+    const size_t wb = ws.size();
+    const int e = call([&] {
+        return api.cache4_attn(rq.p, rq.strides, pc, (const int32_t*)pt, (const int32_t*)pl, (const int32_t*)pn, ro.p, ro.strides, (float*)ps, pw, wb, B, Hq,
+                               c.heads(), Nq, D, type, c.num_pages(), c.columns(), page, group, causal != 0, scale, splits, st);
+    });
+    return lse.t ? result(e, {&o, &lse}) : result(e, {&o});
+}
+
+// (q, cache, pages, lengths, lse, weights | None, count | None, causal, sm_scale | None, page, group, out | None, stream | None)
+PyObject* py_cache4_weights(PyObject* const* argv, Py_ssize_t n) {
+    if (n != 13) return none();
+    ServingArgs a(argv);
+    const at::Tensor* q = a.rows();
+    if (!a.ok) return none();
+    const int64_t B = q->size(0), Hq = q->size(1), Nq = q->size(2), D = q->size(3);
+    CacheOf c;
+    if (!c.read(a, B)) return none();
+    const at::Tensor *lengths = a.flat(I32, {B}), *lse = a.flat(F32, {B, Hq, Nq});
+    const int64_t H = c.heads();
+    const at::Tensor *had = a.flat(F32, {B, H, -1}, true), *count = a.flat(I32, {B}, true);
+    const int causal = a.integer();
+    const bool no_scale = argv[8] == Py_None;
+    const float sm = a.real_or(0.0f);
+    const int page = a.integer(), group = a.integer();
+    const at::Tensor* go = a.flat(F32, {B, H, had ? had->size(2) : -1}, true);
+    void* st = a.stream();
+    if (!a.take(go != nullptr) || !c.form(D, page, group)) return none();
+    const int64_t width = had ? had->size(2) : go ? go->size(2) : (int64_t)c.columns() * page;
+    if (width > 0x7fffffff) return none();
+    Buffer o;
+    o.take(go ? argv[11] : nullptr, *q, {B, H, width}, F32);
+    const RowsOf rq(q);
+    const int type = type_of(*q);
+    const float scale = no_scale ? 1.0f / std::sqrt((float)D) : sm;
+    const void *pc = c.cache->data_ptr(), *pt = c.pages->data_ptr(), *pl = lengths->data_ptr(), *pn = at_or_null(count), *ps = lse->data_ptr(), *ph = at_or_null(had);
+    void* po = o.p();
+    return result(call([&] {
+                      return api.cache4_weights(rq.p, rq.strides, pc, (const int32_t*)pt, (const int32_t*)pl, (const int32_t*)pn, (const float*)ps, (const float*)ph,
+                                                (float*)po, (int)width, B, Hq, H, Nq, D, type, c.num_pages(), c.columns(), page, group, causal != 0, scale, st);
+                  }),
+                  {&o});
+}
+
+// (cache, pages, lengths, weights, out_cache, out_pages, keep, recent, D, page, group, out_weights | None, kept | None, out_lengths | None,
+// stream | None)
+PyObject* py_cache4_evict(PyObject* const* argv, Py_ssize_t n) {
+    if (n != 15) return none();
+    ServingArgs a(argv);
+    CacheOf c, to;
+    if (!c.read(a, -1)) return none();
+    const int64_t B = c.sequences(), H = c.heads();
+    const at::Tensor *lengths = a.flat(I32, {B}), *weights = a.flat(F32, {B, H, -1});
+    if (!to.read(a, B)) return none();
+    const int keep = a.integer(), recent = a.integer(), D = a.integer(), page = a.integer(), group = a.integer();
+    if (!a.ok || keep < 1 || to.heads() != H || !c.form(D, page, group) || !to.form(D, page, group)) return none();
+    const at::Tensor *gw = a.flat(F32, {B, H, -1}, true), *gk = a.flat(I32, {B, H, keep}, true), *gl = a.flat(I32, {B}, true);
+    void* st = a.stream();
+    if (!a.take(gw && gk && gl)) return none();
+    const int64_t out_width = gw ? gw->size(2) : (int64_t)to.columns() * page;
+    if (out_width > 0x7fffffff) return none();
+    Buffer ow, kept, ol;
+    ow.take(gw ? argv[11] : nullptr, *c.cache, {B, H, out_width}, F32);
+    kept.take(gk ? argv[12] : nullptr, *c.cache, {B, H, keep}, I32);
+    ol.take(gl ? argv[13] : nullptr, *c.cache, {B}, I32);
+    const int width = (int)weights->size(2);
+    const void *pc = c.cache->data_ptr(), *pt = c.pages->data_ptr(), *pl = lengths->data_ptr(), *pw = weights->data_ptr(), *qt = to.pages->data_ptr();
+    void *qc = to.cache->data_ptr(), *qw = ow.p(), *qk = kept.p(), *ql = ol.p();
+    return result(call([&] {
+                      return api.cache4_evict(pc, c.num_pages(), (const int32_t*)pt, c.columns(), (const int32_t*)pl, (const float*)pw, width, qc, to.num_pages(),
+                                              (const int32_t*)qt, to.columns(), (float*)qw, (int)out_width, (int32_t*)qk, (int32_t*)ql, B, H, D, page, group, keep,
+                                              recent, st);
+                  }),
+                  {&kept, &ol, &ow});
+}
+
+// (torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, the addresses in Api's order)
 PyObject* py_init(PyObject* const* argv, Py_ssize_t n) {
     constexpr int COUNT = sizeof(Api) / sizeof(void*);
     if (n != 2 + COUNT) {
@@ -364,6 +644,13 @@ PyMethodDef methods[] = {
     {"attn", (PyCFunction)(void (*)(void))guarded<py_attn<false>>, METH_FASTCALL, nullptr},
     {"attn_pv_int8", (PyCFunction)(void (*)(void))guarded<py_attn<true>>, METH_FASTCALL, nullptr},
     {"attention", (PyCFunction)(void (*)(void))guarded<py_attention>, METH_FASTCALL, nullptr},
+    {"rope", (PyCFunction)(void (*)(void))guarded<py_rope<false>>, METH_FASTCALL, nullptr},
+    {"rope_bwd", (PyCFunction)(void (*)(void))guarded<py_rope<true>>, METH_FASTCALL, nullptr},
+    {"cache4_append", (PyCFunction)(void (*)(void))guarded<py_cache4_append>, METH_FASTCALL, nullptr},
+    {"cache4_load", (PyCFunction)(void (*)(void))guarded<py_cache4_load>, METH_FASTCALL, nullptr},
+    {"cache4_attn", (PyCFunction)(void (*)(void))guarded<py_cache4_attn>, METH_FASTCALL, nullptr},
+    {"cache4_weights", (PyCFunction)(void (*)(void))guarded<py_cache4_weights>, METH_FASTCALL, nullptr},
+    {"cache4_evict", (PyCFunction)(void (*)(void))guarded<py_cache4_evict>, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_sage_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

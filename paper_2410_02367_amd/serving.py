@@ -1,5 +1,6 @@
 """Binding of the serving calls of libsage.so (declared in include/sage.h): rotary positions, and the cache of K and V held
-in 4 bits with what works on it.  Argument marshalling only, as in :mod:`binding`, but for sage_rope_frequencies().
+in 4 bits with what works on it.  Argument marshalling only, as in :mod:`binding`, but for sage_rope_frequencies(): the extension
+module makes the calls that are in order, the code here the others, or their errors.
 
 Tensors are [B, H, N, D] with neighbouring channels and any distances between the rows (a transposed view of [B, N, H, D] as a
 projection leaves it is taken as it is); all of a call's tensors are on one device, which need not be the current one."""
@@ -12,7 +13,7 @@ import math
 import torch
 
 from . import binding
-from .binding import SageError, load
+from .binding import SageError, _answer, _fast, _handle, load
 
 _TYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
 _HALVES = (torch.float16, torch.bfloat16)
@@ -162,11 +163,17 @@ def _rope(entry, x, y, positions, inv_freq, interleaved, amplitude, x_out, y_out
 def sage_rope(q, k, positions, inv_freq, interleaved: bool = False, amplitude: float = 1.0, q_out=None, k_out=None, stream=None):
     """q [B,Hq,N,D] and k [B,Hk,N,D] (or None) with their pairs of channels turned by position * inv_freq -> (q', k'), or q'.
     positions int32 [N] or [B,N]; inv_freq fp64 [rotated / 2], the channels from `rotated` on pass; outputs may be the inputs."""
+    r = _fast().rope(q, k, positions, inv_freq, interleaved, amplitude, q_out, k_out, _handle(stream))
+    if r is not None:
+        return _answer(r, "sage_rope")
     return _rope("sage_rope", q, k, positions, inv_freq, interleaved, amplitude, q_out, k_out, stream)
 
 
 def sage_rope_bwd(dq, dk, positions, inv_freq, interleaved: bool = False, amplitude: float = 1.0, dq_out=None, dk_out=None, stream=None):
     """The gradients of sage_rope()'s inputs from those of its outputs, dq [B,Hq,N,D] and dk [B,Hk,N,D] (or None)."""
+    r = _fast().rope_bwd(dq, dk, positions, inv_freq, interleaved, amplitude, dq_out, dk_out, _handle(stream))
+    if r is not None:
+        return _answer(r, "sage_rope_bwd")
     return _rope("sage_rope_bwd", dq, dk, positions, inv_freq, interleaved, amplitude, dq_out, dk_out, stream)
 
 
@@ -192,6 +199,9 @@ def _cache(cache, pages, B, Hkv, D, page, group, device, name="cache", pages_nam
 def sage_cache4_append(k, v, cache, pages, start, count=None, k_mean=None, page: int = 64, group: int = 32, stream=None):
     """New tokens k, v [B,Hkv,N,D] into slots start[b] .. of the sequences' pages, the first count[b] of each; k_mean [B,Hkv,D]
     fp32 is subtracted from the keys.  -> cache"""
+    r = _fast().cache4_append(k, v, cache, pages, start, count, k_mean, page, group, _handle(stream))
+    if r is not None:
+        return _answer(r, "sage_cache4_append")
     _tensor(k, "k", _HALVES, 4)
     if _elsewhere(k.device, stream):
         return _there(k.device, stream, sage_cache4_append, k, v, cache, pages, start, count, k_mean, page, group)
@@ -212,6 +222,10 @@ def sage_cache4_load(cache, pages, start, N: int, D: int, count=None, k_mean=Non
                      k=None, v=None, stream=None):
     """Slots start[b] .. start[b] + N - 1 (start None: from 0) as the values they stand for -> (k, v) [B,Hkv,N,D]; zeros from
     count[b] on and where no token is."""
+    if dtype in _HALVES:
+        r = _fast().cache4_load(cache, pages, start, N, D, count, k_mean, dtype == torch.bfloat16, page, group, k, v, _handle(stream))
+        if r is not None:
+            return _answer(r, "sage_cache4_load")
     _tensor(cache, "cache", (torch.uint8,), 3)
     if _elsewhere(cache.device, stream):
         return _there(cache.device, stream, sage_cache4_load, cache, pages, start, N, D, count, k_mean, dtype, page, group, k, v)
@@ -246,6 +260,10 @@ def sage_cache4_attn(q, cache, pages, lengths, count=None, causal: bool = True, 
     Query head hq reads key head hq / (Hq / Hkv).  A sequence has its first count[b] queries (None: all; the rows behind them
     become zeros), query t being token lengths[b] - count[b] + t, which with the causal mask sees the tokens up to itself.
     workspace: uint8 tensor of at least sage_cache4_attn_workspace(...) bytes (allocated here if not given)."""
+    r = _fast().cache4_attn(q, cache, pages, lengths, count, causal, sm_scale, page, group, n_splits, return_lse, out, lse, workspace,
+                            _handle(stream))
+    if r is not None:
+        return _answer(r, "sage_cache4_attn")
     _tensor(q, "q", _HALVES, 4)
     if _elsewhere(q.device, stream):
         return _there(q.device, stream, sage_cache4_attn, q, cache, pages, lengths, count, causal, sm_scale, page, group, n_splits,
@@ -277,6 +295,9 @@ def sage_cache4_weights(q, cache, pages, lengths, lse, weights=None, count=None,
     """What the queries of sage_cache4_attn() gave to each slot, summed over the queries and the query heads of each key head and
     added to `weights` [B,Hkv,W] fp32 (None: zeros), W at least the tokens that the table has room for -> out, which may be
     `weights` itself.  lse is that call's."""
+    r = _fast().cache4_weights(q, cache, pages, lengths, lse, weights, count, causal, sm_scale, page, group, out, _handle(stream))
+    if r is not None:
+        return _answer(r, "sage_cache4_weights")
     _tensor(q, "q", _HALVES, 4)
     if _elsewhere(q.device, stream):
         return _there(q.device, stream, sage_cache4_weights, q, cache, pages, lengths, lse, weights, count, causal, sm_scale, page, group, out)
@@ -304,6 +325,10 @@ def sage_cache4_evict(cache, pages, lengths, weights, out_pages, keep: int, rece
     weights (ties: the lowest slots); their rows are copied in order into the pages that out_pages [B,columns'] names (of
     out_cache; None: of cache itself), none of which may be one that `pages` names.
     -> (kept [B,Hkv,keep] int32, the slots, then -1; out_lengths [B] int32; out_weights [B,Hkv,W'] fp32, zeros behind)"""
+    r = _fast().cache4_evict(cache, pages, lengths, weights, cache if out_cache is None else out_cache, out_pages, keep, recent, D, page, group,
+                             out_weights, kept, out_lengths, _handle(stream))
+    if r is not None:
+        return _answer(r, "sage_cache4_evict")
     _tensor(cache, "cache", (torch.uint8,), 3)
     if _elsewhere(cache.device, stream):
         return _there(cache.device, stream, sage_cache4_evict, cache, pages, lengths, weights, out_pages, keep, recent, D, page, group,
