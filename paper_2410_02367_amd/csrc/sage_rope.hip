@@ -23,50 +23,143 @@ template <> struct RopeType<float> {
     static __device__ __forceinline__ float put(float x) { return x; }
 };
 
-// One thread per pair of channels (and per pair of channels that pass).
-template <class T>
+// VEC pairs of a token for HEADS heads: both halves of the pairs as vectors (interleaved: 2 VEC neighbouring channels), the angles
+// made once for all heads while the rows are on their way.  Vectors past the rotated channels are copied.
+template <class T, int VEC, int HEADS>
 __global__ void __launch_bounds__(256) rope_kernel(RopeTensor q, RopeTensor k, const int* __restrict__ positions, long position_stride,
                                                    const double* __restrict__ inv_freq, float amplitude, int N, int D, int R,
-                                                   int interleaved, float sign, long total) {
-    const int pairs = D / 2, H = q.H + k.H;
-    for (long w = blockIdx.x * 256l + threadIdx.x; w < total; w += gridDim.x * 256l) {
-        const int i = (int)(w % pairs);
-        long r = w / pairs;
-        const int h = (int)(r % H);
-        r /= H;
-        const int n = (int)(r % N), b = (int)(r / N);
+                                                   int interleaved, float sign, long tokens) {
+    typedef T vec __attribute__((ext_vector_type(VEC)));
+    const int units = D / (2 * VEC), turned = R / (2 * VEC);
+    const long w = blockIdx.x * 256l + threadIdx.x, token = w / units;
+    if (token >= tokens) return;
+    const int j = (int)(w - token * units), b = (int)(token / N), n = (int)(token - (long)b * N);
+    const bool turn = j < turned;
+    // the two vectors of the unit
+    const int first = turn && !interleaved ? VEC * j : 2 * VEC * j, second = turn && !interleaved ? R / 2 + VEC * j : 2 * VEC * j + VEC;
+    vec x0[HEADS], x1[HEADS];
+    T* to[HEADS];
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) {
+        const int h = blockIdx.y * HEADS + i;
+        to[i] = nullptr;
+        if (h >= q.H + k.H) continue;
         const RopeTensor& t = h < q.H ? q : k;
         const int ht = h < q.H ? h : h - q.H;
-        const T* x = (const T*)t.x + b * t.xs.b + ht * t.xs.h + n * t.xs.n;
-        T* y = (T*)t.y + b * t.ys.b + ht * t.ys.h + n * t.ys.n;
-        if (2 * i >= R) {
-            const T u = x[2 * i], v = x[2 * i + 1];
-            y[2 * i] = u;
-            y[2 * i + 1] = v;
-            continue;
-        }
-        // turns, in fp64: far positions are many of them, and only the fraction counts
-        const double turns = positions[b * position_stride + n] * (inv_freq[i] * 0.15915494309189535);
-        const float part = (float)(turns - __builtin_rint(turns));
-        const float c = amplitude * cospif(2.0f * part), s = sign * amplitude * sinpif(2.0f * part);
-        const int c0 = interleaved ? 2 * i : i, c1 = interleaved ? 2 * i + 1 : i + R / 2;
-        const float u = RopeType<T>::get(x[c0]), v = RopeType<T>::get(x[c1]);
-        y[c0] = RopeType<T>::put(u * c - v * s);
-        y[c1] = RopeType<T>::put(v * c + u * s);
+        const T* const x = (const T*)t.x + b * t.xs.b + ht * t.xs.h + n * t.xs.n;
+        to[i] = (T*)t.y + b * t.ys.b + ht * t.ys.h + n * t.ys.n;
+        x0[i] = *(const vec*)(x + first);
+        x1[i] = *(const vec*)(x + second);
     }
+    if (turn) {
+        float c[VEC], s[VEC];
+        const double position = positions[b * position_stride + n] * 0.15915494309189535;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            // turns, in fp64: far positions are many of them, and only the fraction counts
+            const double turns = position * inv_freq[VEC * j + e];
+            sincospif(2.0f * (float)(turns - __builtin_rint(turns)), &s[e], &c[e]);
+            c[e] *= amplitude;
+            s[e] *= sign * amplitude;
+        }
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) {
+            if (interleaved) {
+                vec y0, y1;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float u = RopeType<T>::get(2 * e < VEC ? x0[i][2 * e % VEC] : x1[i][2 * e % VEC]);
+                    const float v = RopeType<T>::get(2 * e < VEC ? x0[i][(2 * e + 1) % VEC] : x1[i][(2 * e + 1) % VEC]);
+                    const T a = RopeType<T>::put(u * c[e] - v * s[e]), d = RopeType<T>::put(v * c[e] + u * s[e]);
+                    if (2 * e < VEC) {
+                        y0[2 * e % VEC] = a;
+                        y0[(2 * e + 1) % VEC] = d;
+                    } else {
+                        y1[2 * e % VEC] = a;
+                        y1[(2 * e + 1) % VEC] = d;
+                    }
+                }
+                x0[i] = y0;
+                x1[i] = y1;
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float u = RopeType<T>::get(x0[i][e]), v = RopeType<T>::get(x1[i][e]);
+                    x0[i][e] = RopeType<T>::put(u * c[e] - v * s[e]);
+                    x1[i][e] = RopeType<T>::put(v * c[e] + u * s[e]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i)
+        if (to[i] != nullptr) {
+            *(vec*)(to[i] + first) = x0[i];
+            *(vec*)(to[i] + second) = x1[i];
+        }
+}
+
+// Pairs that no vector of 4 fits: one thread per pair of channels (and per pair of channels that pass).
+template <class T>
+__global__ void __launch_bounds__(256) rope_pair_kernel(RopeTensor q, RopeTensor k, const int* __restrict__ positions, long position_stride,
+                                                        const double* __restrict__ inv_freq, float amplitude, int N, int D, int R,
+                                                        int interleaved, float sign, long total) {
+    const int pairs = D / 2, H = q.H + k.H;
+    const long w = blockIdx.x * 256l + threadIdx.x;
+    if (w >= total) return;
+    const int i = (int)(w % pairs);
+    long r = w / pairs;
+    const int h = (int)(r % H);
+    r /= H;
+    const int n = (int)(r % N), b = (int)(r / N);
+    const RopeTensor& t = h < q.H ? q : k;
+    const int ht = h < q.H ? h : h - q.H;
+    const T* x = (const T*)t.x + b * t.xs.b + ht * t.xs.h + n * t.xs.n;
+    T* y = (T*)t.y + b * t.ys.b + ht * t.ys.h + n * t.ys.n;
+    if (2 * i >= R) {
+        const T u = x[2 * i], v = x[2 * i + 1];
+        y[2 * i] = u;
+        y[2 * i + 1] = v;
+        return;
+    }
+    const double turns = positions[b * position_stride + n] * 0.15915494309189535 * inv_freq[i];
+    float s, c;
+    sincospif(2.0f * (float)(turns - __builtin_rint(turns)), &s, &c);
+    c *= amplitude;
+    s *= sign * amplitude;
+    const int c0 = interleaved ? 2 * i : i, c1 = interleaved ? 2 * i + 1 : i + R / 2;
+    const float u = RopeType<T>::get(x[c0]), v = RopeType<T>::get(x[c1]);
+    y[c0] = RopeType<T>::put(u * c - v * s);
+    y[c1] = RopeType<T>::put(v * c + u * s);
+}
+
+template <class T>
+static void launch_rope_type(const RopeTensor& q, const RopeTensor& k, const int* positions, long position_stride, const double* inv_freq,
+                             float amplitude, int B, int N, int D, int R, bool interleaved, float sign, hipStream_t st) {
+    const long tokens = (long)B * N;
+    const int H = q.H + k.H;
+#define SAGE_ROPE(VEC, HEADS) rope_kernel<T, VEC, HEADS><<<dim3((unsigned)((tokens * (D / (2 * VEC)) + 255) / 256), (H + HEADS - 1) / HEADS), 256, 0, st>>>( \
+        q, k, positions, position_stride, inv_freq, amplitude, N, D, R, interleaved, sign, tokens)
+    // one head per thread while that leaves no compute unit without work
+    const bool few = tokens * H * (D / 16) < (1l << 17);
+    if (R % 16 == 0 && D % 16 == 0) {
+        if (few) SAGE_ROPE(8, 1); else SAGE_ROPE(8, 4);
+    } else if (R % 8 == 0) {
+        if (few) SAGE_ROPE(4, 1); else SAGE_ROPE(4, 4);
+    } else {
+        const long total = tokens * H * (D / 2);
+        rope_pair_kernel<T><<<(unsigned)((total + 255) / 256), 256, 0, st>>>(q, k, positions, position_stride, inv_freq, amplitude, N, D, R, interleaved,
+                                                                             sign, total);
+    }
+#undef SAGE_ROPE
 }
 
 hipError_t launch_rope(const RopeTensor& q, const RopeTensor& k, const int* positions, long position_stride, const double* inv_freq,
                        float amplitude, int B, int N, int D, int rotated, int type, bool interleaved, bool backward, hipStream_t st) {
-    const long total = (long)B * N * (q.H + k.H) * (D / 2);
-    const long want = (total + 255) / 256;
-    const dim3 grid((unsigned)(want < (1 << 20) ? want : (1 << 20)));
     const float sign = backward ? -1.0f : 1.0f;
-#define SAGE_ROPE(T) rope_kernel<T><<<grid, 256, 0, st>>>(q, k, positions, position_stride, inv_freq, amplitude, N, D, rotated, interleaved, sign, total)
-    if (type == TYPE_F32) SAGE_ROPE(float);
-    else if (type == TYPE_BF16) SAGE_ROPE(__bf16);
-    else SAGE_ROPE(_Float16);
-#undef SAGE_ROPE
+    if (type == TYPE_F32) launch_rope_type<float>(q, k, positions, position_stride, inv_freq, amplitude, B, N, D, rotated, interleaved, sign, st);
+    else if (type == TYPE_BF16) launch_rope_type<__bf16>(q, k, positions, position_stride, inv_freq, amplitude, B, N, D, rotated, interleaved, sign, st);
+    else launch_rope_type<_Float16>(q, k, positions, position_stride, inv_freq, amplitude, B, N, D, rotated, interleaved, sign, st);
     return hipGetLastError();
 }
 
