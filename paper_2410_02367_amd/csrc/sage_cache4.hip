@@ -46,12 +46,6 @@ __device__ __forceinline__ void put_row8(void* p, long at, const float (&x)[8]) 
 }
 // the scale of a group from its largest magnitude
 __device__ __forceinline__ _Float16 scale_of(float amax) { return (_Float16)__builtin_fminf(amax / 7.0f, MAX_SCALE); }
-// nibble of x; a NaN is stored as 0, infinities saturate
-__device__ __forceinline__ unsigned nibble(float x, float delta) {
-    const float c = __builtin_rintf(x / delta);
-    const float r = __builtin_fminf(__builtin_fmaxf(c, -7.0f), 7.0f);
-    return delta > 0.0f && x == x ? (unsigned)((int)r + 8) : 8u;
-}
 // where channel e of 8 stands in its word
 template <bool IS_K> __device__ __forceinline__ int nibble_shift(int e) { return IS_K ? 4 * (e >> 1) + 16 * (e & 1) : 4 * e; }
 // the word of octet o (channels 8 o .. 8 o + 7) in its row
@@ -64,12 +58,36 @@ __device__ __forceinline__ float group_max(const float (&x)[8]) {
     for (int e = 0; e < 8; ++e) m = __builtin_fmaxf(m, __builtin_fabsf(x[e]));
     return lanes_max<GROUP / 8>(m);
 }
+// The codes of 8 channels in their word.  The quotient x / delta to the last bit by three instructions per channel instead of a
+// division's ten (which were most of the call): with y = 1 / delta correctly rounded, q = x y is off by an ulp at most, its
+// remainder x - q delta is exact in an FMA, and q + remainder y rounds to the quotient.  Limited to 8 steps before that, so that
+// infinities saturate and nothing overflows; the addition of 1.5 * 2^23 + 8 rounds to whole numbers, ties to even, and leaves
+// code + 8 in the low bits.
 template <bool IS_K>
 __device__ __forceinline__ unsigned pack8(const float (&x)[8], float delta) {
-    unsigned w = 0;
+    const float y = delta > 0.0f ? 1.0f / delta : 0.0f, most = 8.0f * delta;
+    unsigned n[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w |= nibble(x[e], delta) << nibble_shift<IS_K>(e);
-    return w;
+    for (int e = 0; e < 8; ++e) {
+        const float z = __builtin_amdgcn_fmed3f(x[e], -most, most), q = z * y;
+        const float exact = __builtin_fmaf(__builtin_fmaf(-q, delta, z), y, q);
+        n[e] = __builtin_bit_cast(unsigned, __builtin_amdgcn_fmed3f(exact, -7.0f, 7.0f) + 12582920.0f);
+    }
+    // two nibbles in the low byte of a word, four of those to a word
+    auto pair = [&n](int i, int j) { return (n[i] & 15u) | n[j] << 4; };
+    const unsigned b0 = IS_K ? pair(0, 2) : pair(0, 1), b1 = IS_K ? pair(4, 6) : pair(2, 3);
+    const unsigned b2 = IS_K ? pair(1, 3) : pair(4, 5), b3 = IS_K ? pair(5, 7) : pair(6, 7);
+    return __builtin_amdgcn_perm(b1, b0, 0x0c0c0400u) | __builtin_amdgcn_perm(b3, b2, 0x04000c0cu);
+}
+// NaN to 0
+__device__ __forceinline__ void numbers(float (&x)[8]) {
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) odd |= __builtin_isunordered(x[e], x[e + 1]);
+    if (__builtin_expect(odd, 0)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = x[e] == x[e] ? x[e] : 0.0f;
+    }
 }
 template <bool IS_K>
 __device__ __forceinline__ void unpack8(unsigned w, float delta, float (&x)[8]) {
@@ -101,6 +119,8 @@ __global__ void __launch_bounds__(256) cache4_append_kernel(Cache4 c, const void
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] -= k_mean[(size_t)bh * D + 8 * o + e];
     }
+    numbers(x);
+    numbers(y);
     const _Float16 dk = scale_of(group_max<GROUP>(x)), dv = scale_of(group_max<GROUP>(y));
     ((unsigned*)(block + c.k_codes(r)))[octet_word<true>(o, D)] = pack8<true>(x, (float)dk);
     ((unsigned*)(block + c.v_codes(r)))[octet_word<false>(o, D)] = pack8<false>(y, (float)dv);
@@ -166,24 +186,26 @@ hipError_t launch_cache4_load(const Cache4& c, const int* start, const int* coun
 
 // ---- eviction
 // The slots that stay, in order: the last `recent` of n and, of the m before them, the need = keep - recent with the largest
-// weights, of equal ones the lowest slots.  One workgroup per (sequence, head).  The need-th largest weight is found a byte at
-// a time from the top (a histogram of the weights that share the bytes found so far); then every wavefront counts, in a share
-// of the slots of its own, those above it and those equal to it, and writes its share.
+// weights, of equal ones the lowest slots.  One workgroup per (sequence, head); a wavefront has a share of the slots of its
+// own, the first 1024 of them in registers.  The need-th largest weight is found 11, 11 and 10 bits at a time from the top: a
+// histogram of the weights that share the bits found so far, and a sum over the bins from the largest down.  Then every
+// wavefront counts those of its share above it and equal to it, and writes its share.
 namespace {
 // larger weight, larger key; a NaN below all numbers, -0 with 0
 __device__ __forceinline__ unsigned rank_key(float w) {
     const unsigned u = __builtin_bit_cast(unsigned, w + 0.0f);
     return w != w ? 0u : (u >> 31 ? ~u : u | 0x80000000u);
 }
+__device__ __forceinline__ int popcount(unsigned long long x) { return __builtin_popcountll(x); }
 }  // namespace
 
-constexpr int SELECT_NT = 1024, SELECT_WAVES = SELECT_NT / 64;
+constexpr int SELECT_NT = 1024, SELECT_WAVES = SELECT_NT / 64, SELECT_HELD = 16, SELECT_BINS = 2048;
 __global__ void __launch_bounds__(SELECT_NT) cache4_select_kernel(const int* __restrict__ lengths, const float* __restrict__ weights, int width,
                                                                   int capacity, int heads, int* __restrict__ kept,
                                                                   int* __restrict__ out_lengths, int keep, int recent) {
-    __shared__ int histogram[256];
-    __shared__ int s_digit, s_above, s_gt[SELECT_WAVES], s_eq[SELECT_WAVES];
-    const int bh = blockIdx.x, b = bh / heads, t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    __shared__ int histogram[SELECT_BINS];
+    __shared__ int s_digit, s_above, s_total[SELECT_WAVES], s_gt[SELECT_WAVES], s_eq[SELECT_WAVES];
+    const int bh = blockIdx.x, b = bh / heads, t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int n = min(max(lengths[b], 0), capacity);
     int* const to = kept + (size_t)bh * keep;
     if (bh == b * heads && t == 0) out_lengths[b] = min(n, keep);
@@ -195,34 +217,78 @@ __global__ void __launch_bounds__(SELECT_NT) cache4_select_kernel(const int* __r
     const int m = n - recent, need = keep - recent;
     for (int i = t; i < recent; i += SELECT_NT) to[need + i] = m + i;
     if (need == 0) return;
+    const int share = (m + SELECT_NT - 1) / SELECT_NT * 64, first = min(wave * share, m), last = min(first + share, m);
+    unsigned held[SELECT_HELD];
+#pragma unroll
+    for (int j = 0; j < SELECT_HELD; ++j) {
+        const int i = first + 64 * j + lane;
+        held[j] = i < last ? rank_key(w[i]) : 0u;
+    }
+    // f(key, slot, whether there is one) for the lane's slots, 64 neighbouring ones of the wavefront at a time
+    auto walk = [&](auto&& f) {
+#pragma unroll
+        for (int j = 0; j < SELECT_HELD; ++j)
+            if (first + 64 * j < last) f(held[j], first + 64 * j + lane, first + 64 * j + lane < last);
+        for (int i0 = first + 64 * SELECT_HELD; i0 < last; i0 += 64 * 4) {
+            float x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = w[min(i0 + 64 * j + lane, m - 1)];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (i0 + 64 * j < last) f(rank_key(x[j]), i0 + 64 * j + lane, i0 + 64 * j + lane < last);
+        }
+    };
     unsigned found = 0, mask = 0;
     int left = need;                    // of the keys that match `found` under `mask`, how many stay
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (t < 256) histogram[t] = 0;
+#pragma unroll
+    for (int step = 0; step < 3; ++step) {
+        const int shift = step == 0 ? 21 : step == 1 ? 10 : 0;
+        const unsigned bins = step == 2 ? 1023u : 2047u;
+        histogram[t] = 0;
+        histogram[t + SELECT_NT] = 0;
         __syncthreads();
-        for (int i = t; i < m; i += SELECT_NT) {
-            const unsigned u = rank_key(w[i]);
-            if ((u & mask) == found) atomicAdd(&histogram[u >> shift & 255u], 1);
+        walk([&](unsigned u, int, bool is) {
+            const bool counts = is && (u & mask) == found;
+            const unsigned long long all = __builtin_amdgcn_ballot_w64(counts);
+            if (all == 0) return;
+            // equal keys are common (zeros): one addition for the wavefront
+            const unsigned d = u >> shift & bins, one = __builtin_amdgcn_readlane(d, __builtin_ctzll(all));
+            if (__builtin_amdgcn_ballot_w64(counts && d != one) == 0) {
+                if (lane == 0) atomicAdd(&histogram[one], popcount(all));
+            } else if (counts) {
+                atomicAdd(&histogram[d], 1);
+            }
+        });
+        __syncthreads();
+        // thread t: bins 2 t and 2 t + 1; `above`: keys in the bins after them
+        const int h0 = histogram[2 * t], h1 = histogram[2 * t + 1];
+        int above = h0 + h1;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int x = __shfl_down(above, off, 64);
+            above += lane + off < 64 ? x : 0;
         }
+        if (lane == 0) s_total[wave] = above;
         __syncthreads();
-        if (t == 0) {
-            int above = 0, d = 255;
-            while (d > 0 && above + histogram[d] < left) above += histogram[d--];
-            s_digit = d;
+        above -= h0 + h1;
+        for (int i = wave + 1; i < SELECT_WAVES; ++i) above += s_total[i];
+        if (above < left && left <= above + h1) {
+            s_digit = 2 * t + 1;
             s_above = above;
+        } else if (above + h1 < left && left <= above + h1 + h0) {
+            s_digit = 2 * t;
+            s_above = above + h1;
         }
         __syncthreads();
         found |= (unsigned)s_digit << shift;
-        mask |= 255u << shift;
+        mask |= bins << shift;
         left -= s_above;
     }
-    const int share = (m + SELECT_WAVES * 64 - 1) / (SELECT_WAVES * 64) * 64, first = min(wave * share, m), last = min(first + share, m);
     int gt = 0, eq = 0;
-    for (int i = first + lane; i - lane < last; i += 64) {
-        const unsigned u = i < last ? rank_key(w[i]) : 0u;
-        gt += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < last && u > found));
-        eq += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < last && u == found));
-    }
+    walk([&](unsigned u, int, bool is) {
+        gt += popcount(__builtin_amdgcn_ballot_w64(is && u > found));
+        eq += popcount(__builtin_amdgcn_ballot_w64(is && u == found));
+    });
     if (lane == 0) {
         s_gt[wave] = gt;
         s_eq[wave] = eq;
@@ -234,41 +300,65 @@ __global__ void __launch_bounds__(SELECT_NT) cache4_select_kernel(const int* __r
         ties += s_eq[i];
     }
     at += min(ties, left);
-    for (int i = first + lane; i - lane < last; i += 64) {
-        const unsigned u = i < last ? rank_key(w[i]) : 0u;
-        const unsigned long long equal = __builtin_amdgcn_ballot_w64(i < last && u == found), below = (1ull << lane) - 1ull;
-        const bool stays = i < last && (u > found || (u == found && ties + __builtin_popcountll(equal & below) < left));
+    walk([&](unsigned u, int i, bool is) {
+        const unsigned long long equal = __builtin_amdgcn_ballot_w64(is && u == found), below = (1ull << lane) - 1ull;
+        const bool stays = is && (u > found || (u == found && ties + popcount(equal & below) < left));
         const unsigned long long all = __builtin_amdgcn_ballot_w64(stays);
-        if (stays) to[at + __builtin_popcountll(all & below)] = i;
-        at += __builtin_popcountll(all);
-        ties += __builtin_popcountll(equal);
-    }
+        if (stays) to[at + popcount(all & below)] = i;
+        at += popcount(all);
+        ties += popcount(equal);
+    });
 }
 
 // The kept rows copied: D / 32 threads for 16 bytes each of the K codes, as many for V's; each also one of the 2 D / group
-// scales.  A row whose page holds no tokens becomes zeros.
+// scales.  A row whose page holds no tokens becomes zeros.  A thread has GATHER_ROWS rows: index, pages and bytes are three
+// round trips to memory, one after the other.
+constexpr int GATHER_ROWS = 4;
 template <int D>
 __global__ void __launch_bounds__(256) cache4_gather_kernel(Cache4 c, Cache4 to, const int* __restrict__ kept, const float* __restrict__ weights,
                                                             int width, float* __restrict__ out_weights, int out_width, int keep) {
     constexpr int TPR = D / 16, ROWS = 256 / TPR;
     typedef unsigned u4 __attribute__((ext_vector_type(4)));
     const int bh = blockIdx.y, b = bh / c.heads, h = bh - b * c.heads, i = threadIdx.x % TPR;
-    const int j = blockIdx.x * ROWS + threadIdx.x / TPR;
-    const int from = j < keep ? kept[(size_t)bh * keep + j] : -1;
-    if (i == 0 && j < out_width) out_weights[(size_t)bh * out_width + j] = from >= 0 ? weights[(size_t)bh * width + from] : 0.0f;
-    if (from < 0) return;
-    unsigned char* const dst = to.block(b, h, j);
-    if (dst == nullptr) return;
-    const unsigned char* const src = c.block(b, h, from);
-    const int rs = from & (c.page() - 1), rd = j & (to.page() - 1), S = c.scales();
-    const bool is_v = i >= TPR / 2;
-    const int chunk = is_v ? i - TPR / 2 : i;
-    const u4 x = src != nullptr ? ((const u4*)(src + (is_v ? c.v_codes(rs) : c.k_codes(rs))))[chunk]
-                                : (u4){0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u};
-    ((u4*)(dst + (is_v ? to.v_codes(rd) : to.k_codes(rd))))[chunk] = x;
-    if (chunk < S) {
-        const unsigned short s = src != nullptr ? ((const unsigned short*)(src + (is_v ? c.v_scales(rs) : c.k_scales(rs))))[chunk] : 0;
-        ((unsigned short*)(dst + (is_v ? to.v_scales(rd) : to.k_scales(rd))))[chunk] = s;
+    const int j0 = blockIdx.x * ROWS * GATHER_ROWS + threadIdx.x / TPR, S = c.scales(), half = D / 32;
+    const bool is_v = i >= half;
+    const int chunk = is_v ? i - half : i;
+    int from[GATHER_ROWS];
+#pragma unroll
+    for (int r = 0; r < GATHER_ROWS; ++r) {
+        const int j = j0 + r * ROWS;
+        from[r] = j < keep ? kept[(size_t)bh * keep + j] : -1;
+    }
+    const unsigned char* src[GATHER_ROWS];
+    unsigned char* dst[GATHER_ROWS];
+#pragma unroll
+    for (int r = 0; r < GATHER_ROWS; ++r) {
+        src[r] = from[r] >= 0 ? c.block(b, h, from[r]) : nullptr;
+        dst[r] = from[r] >= 0 ? to.block(b, h, j0 + r * ROWS) : nullptr;
+    }
+    u4 x[GATHER_ROWS];
+    unsigned short s[GATHER_ROWS];
+    float w[GATHER_ROWS];
+#pragma unroll
+    for (int r = 0; r < GATHER_ROWS; ++r) {
+        x[r] = (u4){0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u};
+        s[r] = 0;
+        w[r] = 0.0f;
+        const int row = from[r] & (c.page() - 1);
+        if (src[r] != nullptr) {
+            x[r] = ((const u4*)(src[r] + (is_v ? c.v_codes(row) : c.k_codes(row))))[chunk];
+            if (chunk < S) s[r] = ((const unsigned short*)(src[r] + (is_v ? c.v_scales(row) : c.k_scales(row))))[chunk];
+        }
+        if (i == 0 && from[r] >= 0) w[r] = weights[(size_t)bh * width + from[r]];
+    }
+#pragma unroll
+    for (int r = 0; r < GATHER_ROWS; ++r) {
+        const int j = j0 + r * ROWS, row = j & (to.page() - 1);
+        if (i == 0 && j < out_width) out_weights[(size_t)bh * out_width + j] = w[r];
+        if (dst[r] != nullptr) {
+            ((u4*)(dst[r] + (is_v ? to.v_codes(row) : to.k_codes(row))))[chunk] = x[r];
+            if (chunk < S) ((unsigned short*)(dst[r] + (is_v ? to.v_scales(row) : to.k_scales(row))))[chunk] = s[r];
+        }
     }
 }
 
@@ -276,7 +366,7 @@ hipError_t launch_cache4_evict(const Cache4& c, const int* lengths, const float*
                                int out_width, int* kept, int* out_lengths, int B, int keep, int recent, hipStream_t st) {
     cache4_select_kernel<<<B * c.heads, SELECT_NT, 0, st>>>(lengths, weights, width, c.capacity(), c.heads, kept, out_lengths, keep, recent);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    const int rows = 256 / (c.D / 16);
+    const int rows = 256 / (c.D / 16) * GATHER_ROWS;
     const dim3 grid((out_width + rows - 1) / rows, B * c.heads);
     if (c.D == 64) cache4_gather_kernel<64><<<grid, 256, 0, st>>>(c, to, kept, weights, width, out_weights, out_width, keep);
     else cache4_gather_kernel<128><<<grid, 256, 0, st>>>(c, to, kept, weights, width, out_weights, out_width, keep);
