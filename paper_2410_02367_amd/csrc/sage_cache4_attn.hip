@@ -593,77 +593,187 @@ __global__ void __launch_bounds__(256) cache4_merge_kernel(Cache4 c, CacheQuerie
     }
 }
 
-// A workgroup takes 256 keys of a (sequence, head), a wavefront 64 of them, whose operands stay in its registers while it walks
-// the rows 16 at a time; a lane's sums belong to 16 keys and one column of rows, and the columns are added at the end.
+// ---- the weights of the keys
+namespace {
+// the sum over the 16 columns of rows, in all of them
+__device__ __forceinline__ float over_columns(float x) {
+    auto rotated = [](float y, auto CTRL) {
+        const int v = __builtin_bit_cast(int, y);
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(v, v, decltype(CTRL)::value, 0xF, 0xF, false));
+    };
+    x += rotated(x, std::integral_constant<int, 0x128>{});
+    x += rotated(x, std::integral_constant<int, 0x124>{});
+    x += rotated(x, std::integral_constant<int, 0x122>{});
+    return x + rotated(x, std::integral_constant<int, 0x121>{});
+}
+// a row's lse as the base-2 reference its weights are relative to; of a row that saw nothing one that leaves no weight
+__device__ __forceinline__ float row_reference(float lse) { return lse == -__builtin_inff() ? __builtin_inff() : lse * LOG2E; }
+
+// the words and scales of 64 keys as operands
 template <int D, int NG>
-__global__ void __launch_bounds__(WAVES * 64) cache4_weights_kernel(Cache4 c, CacheQueries q, const float* __restrict__ lse,
-                                                                    const float* __restrict__ weights, float* __restrict__ out, int width) {
-    __shared__ __attribute__((aligned(16))) _Float16 s_ks[WAVES][TILE * NG];
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
-    const int slab = blockIdx.y, b = slab / c.heads, head = slab - b * c.heads, share = q.Hq / c.heads;
-    const int k0 = (blockIdx.x * WAVES + wave) * TILE;
-    if (k0 >= width) return;
-    const RowRange range(c, q, b, share);
-    float sum[4][4] = {};
-    const int last_end = range.rows > 0 ? range.end(range.count - 1, q.causal) : 0;
-    if (k0 < last_end) {
-        PageIds pages;
-        pages.look_up(c, c.table + (size_t)b * c.columns, k0);
-        KeyTile<D, NG, false> tile;
-        tile.request(c, c.data + head * c.block_bytes(), pages, k0, lane);
-        *(typename ScaleWord<NG>::type*)(s_ks[wave] + lane * NG) = tile.ks;
-        wave_order();
-        half8 k[4][D / 32];
-        unsigned ks[4][2 * NG];
+struct KeyOperands {
+    half8 k[4][D / 32];
+    unsigned ks[4][2 * NG];
+    // `staged`: the scales of the wavefront's keys, [key][group]
+    __device__ __forceinline__ void make(const KeyTile<D, NG, false>& tile, const _Float16* staged, int h) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             typedef unsigned scales_t __attribute__((ext_vector_type(2 * NG)));
-            const scales_t a = *(const scales_t*)(s_ks[wave] + (16 * j + 4 * h) * NG);
+            const scales_t a = *(const scales_t*)(staged + (16 * j + 4 * h) * NG);
 #pragma unroll
             for (int e = 0; e < 2 * NG; ++e) ks[j][e] = a[e];
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) k[j][i] = operand(tile.k[j][i]);
         }
-        for (int row0 = 0; row0 < range.rows; row0 += 16) {
-            const int row = min(row0 + col, range.rows - 1), tq = row / share, g = row - tq * share;
-            const int end = row0 + col < range.rows ? range.end(tq, q.causal) : 0;
-            if (range.end(min(row0 + 15, range.rows - 1) / share, q.causal) <= k0) continue;
-            Queries4<D> query;
-            const float sc = query.load(q, b * q.strides.b + (head * share + g) * q.strides.h + tq * q.strides.n, h);
-            float L = lse[((size_t)b * q.Hq + head * share + g) * q.Nq + tq] * LOG2E;
-            if (L == -__builtin_inff()) L = __builtin_inff();
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const c4f s = scores<D, NG>(k[j], query.op, ks[j]);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, -L));
-                    sum[j][r] += k0 + 16 * j + 4 * h + r < end ? p : 0.0f;
-                }
-            }
-        }
-        // the 16 columns of rows
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float x = sum[j][r];
-#pragma unroll
-                for (int off = 8; off; off >>= 1) x += __shfl_xor(x, off, 64);
-                sum[j][r] = tile.bad >> j & 1 ? 0.0f : x;
-            }
     }
-    // lane (col, h) writes key 16 (col / 4) + 4 h + col % 4
-    float mine = 0.0f;
+};
+// sum[j][r] += the weights that 16 rows give to key 16 j + 4 h + r of a tile; end: slots that the lane's row sees, from k0 on
+template <int D, int NG>
+__device__ __forceinline__ void add_weights(float (&sum)[4][4], const KeyOperands<D, NG>& keys, const half8 (&q)[D / 32], float sc, float reference,
+                                            int end, bool whole, int h) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const c4f s = scores<D, NG>(keys.k[j], q, keys.ks[j]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, -reference));
+            sum[j][r] += whole || 16 * j + 4 * h + r < end ? p : 0.0f;
+        }
+    }
+}
+// adds up the columns and writes the 64 sums
+__device__ __forceinline__ void put_weights(float (&sum)[4][4], unsigned bad, const float* had, float* out, int k0, int width, int lane) {
+    const int col = lane & 15, h = lane >> 4;
+    float mine[4] = {};
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) mine = col == 4 * j + r ? sum[j][r] : mine;
-    const int key = k0 + 16 * (col >> 2) + 4 * h + (col & 3);
-    if (key < width) {
-        const size_t at = (size_t)slab * width + key;
-        out[at] = (weights != nullptr ? weights[at] : 0.0f) + mine;
+        for (int r = 0; r < 4; ++r) {
+            const float x = over_columns(sum[j][r]);
+            mine[r] = col == j ? x : mine[r];
+        }
+    // lanes col < 4: keys 16 col + 4 h ..
+    if (col >= 4) return;
+    const int key = k0 + 16 * col + 4 * h;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        if (key + r < width) out[key + r] = (had != nullptr ? had[key + r] : 0.0f) + (bad >> col & 1 ? 0.0f : mine[r]);
+}
+}  // namespace
+
+// At most 16 rows (a decoding step): their operands stay in registers, a wavefront walks tiles of keys, the next one on its way.
+template <int D, int NG>
+__global__ void __launch_bounds__(WAVES * 64) cache4_weights_few_kernel(Cache4 c, CacheQueries q, const float* __restrict__ lse,
+                                                                        const float* __restrict__ weights, float* __restrict__ out, int width, int chunk) {
+    __shared__ __attribute__((aligned(16))) _Float16 s_ks[WAVES][TILE * NG];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
+    const int slab = blockIdx.y, b = slab / c.heads, head = slab - b * c.heads, share = q.Hq / c.heads;
+    const RowRange range(c, q, b, share);
+    const int last_end = range.rows > 0 ? range.end(range.count - 1, q.causal) : 0;
+    const float* const had = weights != nullptr ? weights + (size_t)slab * width : nullptr;
+    float* const to = out + (size_t)slab * width;
+    constexpr int NEXT = TILE * WAVES;
+    const int k_end = min((int)(blockIdx.x + 1) * chunk, width), seen = min(k_end, last_end);
+    int k0 = blockIdx.x * chunk + TILE * wave;
+    typedef KeyTile<D, NG, false> Tile;
+    Tile tile;
+    PageIds pages;
+    const int* const table = c.table + (size_t)b * c.columns;
+    const unsigned char* const head_at = c.data + head * c.block_bytes();
+    if (k0 < seen) {
+        pages.look_up(c, table, k0);
+        tile.request(c, head_at, pages, k0, lane);
+        pages.look_up(c, table, k0 + NEXT);
+        const int row = min(col, range.rows - 1), tq = row / share, g = row - tq * share;
+        const int end = col < range.rows ? range.end(tq, q.causal) : 0;
+        const int first_end = range.end(0, q.causal);
+        Queries4<D> query;
+        const float sc = query.load(q, b * q.strides.b + (head * share + g) * q.strides.h + tq * q.strides.n, h);
+        // (columns without a row leave no weight either)
+        const float reference = col < range.rows ? row_reference(lse[((size_t)b * q.Hq + head * share + g) * q.Nq + tq]) : __builtin_inff();
+        for (; k0 < seen; k0 += NEXT) {
+            wave_order();
+            *(typename Tile::scale_t*)(s_ks[wave] + lane * NG) = tile.ks;
+            wave_order();
+            KeyOperands<D, NG> keys;
+            keys.make(tile, s_ks[wave], h);
+            const unsigned bad = tile.bad;
+            if (k0 + NEXT < seen) {
+                tile.request(c, head_at, pages, k0 + NEXT, lane);
+                pages.look_up(c, table, k0 + 2 * NEXT);
+            }
+            float sum[4][4] = {};
+            add_weights<D, NG>(sum, keys, query.op, sc, reference, end - k0, k0 + TILE <= first_end, h);
+            put_weights(sum, bad, had, to, k0, width, lane);
+        }
     }
+    // slots that no query sees keep what they had
+    for (; k0 < k_end; k0 += NEXT) {
+        const int key = k0 + lane;
+        if (key < width) to[key] = had != nullptr ? had[key] : 0.0f;
+    }
+}
+
+// More rows: a workgroup takes 256 keys, a wavefront 64 of them, whose operands stay in its registers.  The rows come 64 at a time:
+// each wavefront makes the operands of 16 of them in LDS, and all use them.
+template <int D, int NG>
+__global__ void __launch_bounds__(WAVES * 64, 2) cache4_weights_kernel(Cache4 c, CacheQueries q, const float* __restrict__ lse,
+                                                                       const float* __restrict__ weights, float* __restrict__ out, int width) {
+    __shared__ __attribute__((aligned(16))) _Float16 s_ks[WAVES][TILE * NG];
+    __shared__ half8 s_q[WAVES][D / 32][64];
+    __shared__ float s_sc[WAVES][16], s_reference[WAVES][16];
+    __shared__ int s_end[WAVES][16];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
+    const int slab = blockIdx.y, b = slab / c.heads, head = slab - b * c.heads, share = q.Hq / c.heads;
+    const RowRange range(c, q, b, share);
+    const int last_end = range.rows > 0 ? range.end(range.count - 1, q.causal) : 0;
+    const float* const had = weights != nullptr ? weights + (size_t)slab * width : nullptr;
+    float* const to = out + (size_t)slab * width;
+    const int k_first = blockIdx.x * WAVES * TILE, k0 = k_first + wave * TILE;
+    float sum[4][4] = {};
+    unsigned bad = 0;
+    if (k_first < last_end) {                   // (the same for the whole workgroup)
+        KeyOperands<D, NG> keys;
+        {
+            PageIds pages;
+            pages.look_up(c, c.table + (size_t)b * c.columns, k0);
+            KeyTile<D, NG, false> tile;
+            tile.request(c, c.data + head * c.block_bytes(), pages, k0, lane);
+            *(typename ScaleWord<NG>::type*)(s_ks[wave] + lane * NG) = tile.ks;
+            bad = tile.bad;
+            wave_order();
+            keys.make(tile, s_ks[wave], h);
+        }
+        // the first row that sees a key of the workgroup
+        int row0 = 0;
+        if (q.causal) row0 = max(0, k_first + 1 - (range.length - range.count + 1)) * share / 64 * 64;
+        for (; row0 < range.rows; row0 += 64) {
+            {
+                const int at = row0 + 16 * wave + col, row = min(at, range.rows - 1), tq = row / share, g = row - tq * share;
+                Queries4<D> query;
+                const float sc = query.load(q, b * q.strides.b + (head * share + g) * q.strides.h + tq * q.strides.n, h);
+                __syncthreads();                // the rows before have been read
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) s_q[wave][i][lane] = query.op[i];
+                if (h == 0) {
+                    s_sc[wave][col] = sc;
+                    s_reference[wave][col] = at < range.rows ? row_reference(lse[((size_t)b * q.Hq + head * share + g) * q.Nq + tq]) : __builtin_inff();
+                    s_end[wave][col] = at < range.rows ? range.end(tq, q.causal) : 0;
+                }
+                __syncthreads();
+            }
+#pragma unroll 1
+            for (int w = 0; w < WAVES; ++w) {
+                if (row0 + 16 * w >= range.rows) break;
+                const int first_end = range.end((row0 + 16 * w) / share, q.causal);
+                half8 op[D / 32];
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) op[i] = s_q[w][i][lane];
+                add_weights<D, NG>(sum, keys, op, s_sc[w][col], s_reference[w][col], s_end[w][col] - k0, k0 + TILE <= first_end, h);
+            }
+        }
+    }
+    if (k0 < width) put_weights(sum, bad, had, to, k0, width, lane);
 }
 
 namespace {
@@ -674,7 +784,7 @@ namespace {
 struct AttnPlan {
     int qt, tiles, n_splits, chunk;
 };
-constexpr int WANTED = 512;
+constexpr int WANTED = 512, WANTED_FEW = 1024;
 AttnPlan plan(int B, int Hq, int Hkv, int Nq, int capacity, int requested) {
     const int rows = Hq / Hkv * Nq;
     AttnPlan p;
@@ -732,9 +842,19 @@ hipError_t launch_cache4_attn(const Cache4& c, const CacheQueries& q, void* out,
 
 hipError_t launch_cache4_weights(const Cache4& c, const CacheQueries& q, const float* lse, const float* weights, float* out, int width,
                                  hipStream_t st) {
-    const dim3 grid((width + WAVES * TILE - 1) / (WAVES * TILE), q.B * c.heads);
-    const int ng = c.scales();
-#define SAGE_CACHE4_WEIGHTS(D, NG) cache4_weights_kernel<D, NG><<<grid, WAVES * 64, 0, st>>>(c, q, lse, weights, out, width)
+    const int slabs = q.B * c.heads, ng = c.scales(), tiles = (width + WAVES * TILE - 1) / (WAVES * TILE);
+    const bool few = q.Hq / c.heads * q.Nq <= 16;
+    // few rows: as many workgroups as the attention has, so that a wavefront has tiles to walk
+    int chunks = few ? WANTED_FEW / slabs : tiles;
+    if (chunks < 1) chunks = 1;
+    if (chunks > tiles) chunks = tiles;
+    const int chunk = (tiles + chunks - 1) / chunks * WAVES * TILE;
+    const dim3 grid((width + chunk - 1) / chunk, slabs);
+#define SAGE_CACHE4_WEIGHTS(D, NG)                                                                                          \
+    do {                                                                                                                     \
+        if (few) cache4_weights_few_kernel<D, NG><<<grid, WAVES * 64, 0, st>>>(c, q, lse, weights, out, width, chunk);        \
+        else cache4_weights_kernel<D, NG><<<grid, WAVES * 64, 0, st>>>(c, q, lse, weights, out, width);                       \
+    } while (0)
     if (c.D == 64 && ng == 1) SAGE_CACHE4_WEIGHTS(64, 1);
     else if (c.D == 64) SAGE_CACHE4_WEIGHTS(64, 2);
     else if (ng == 1) SAGE_CACHE4_WEIGHTS(128, 1);
