@@ -199,11 +199,12 @@ __device__ __forceinline__ unsigned rank_key(float w) {
 __device__ __forceinline__ int popcount(unsigned long long x) { return __builtin_popcountll(x); }
 }  // namespace
 
-constexpr int SELECT_NT = 1024, SELECT_WAVES = SELECT_NT / 64, SELECT_HELD = 16, SELECT_BINS = 2048;
+constexpr int SELECT_NT = 1024, SELECT_WAVES = SELECT_NT / 64, SELECT_HELD = 16, SELECT_BINS = 2048, SELECT_COPIES = 4;
 __global__ void __launch_bounds__(SELECT_NT) cache4_select_kernel(const int* __restrict__ lengths, const float* __restrict__ weights, int width,
                                                                   int capacity, int heads, int* __restrict__ kept,
                                                                   int* __restrict__ out_lengths, int keep, int recent) {
-    __shared__ int histogram[SELECT_BINS];
+    // (copies, one for every fourth lane: weights of like size fall into few bins, and additions to one word wait for each other)
+    __shared__ int histogram[SELECT_COPIES][SELECT_BINS + 8];
     __shared__ int s_digit, s_above, s_total[SELECT_WAVES], s_gt[SELECT_WAVES], s_eq[SELECT_WAVES];
     const int bh = blockIdx.x, b = bh / heads, t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int n = min(max(lengths[b], 0), capacity);
@@ -244,8 +245,8 @@ __global__ void __launch_bounds__(SELECT_NT) cache4_select_kernel(const int* __r
     for (int step = 0; step < 3; ++step) {
         const int shift = step == 0 ? 21 : step == 1 ? 10 : 0;
         const unsigned bins = step == 2 ? 1023u : 2047u;
-        histogram[t] = 0;
-        histogram[t + SELECT_NT] = 0;
+#pragma unroll
+        for (int i = 0; i < SELECT_COPIES; ++i) histogram[i][t] = histogram[i][t + SELECT_NT] = 0;
         __syncthreads();
         walk([&](unsigned u, int, bool is) {
             const bool counts = is && (u & mask) == found;
@@ -254,14 +255,19 @@ __global__ void __launch_bounds__(SELECT_NT) cache4_select_kernel(const int* __r
             // equal keys are common (zeros): one addition for the wavefront
             const unsigned d = u >> shift & bins, one = __builtin_amdgcn_readlane(d, __builtin_ctzll(all));
             if (__builtin_amdgcn_ballot_w64(counts && d != one) == 0) {
-                if (lane == 0) atomicAdd(&histogram[one], popcount(all));
+                if (lane == 0) atomicAdd(&histogram[0][one], popcount(all));
             } else if (counts) {
-                atomicAdd(&histogram[d], 1);
+                atomicAdd(&histogram[lane % SELECT_COPIES][d], 1);
             }
         });
         __syncthreads();
         // thread t: bins 2 t and 2 t + 1; `above`: keys in the bins after them
-        const int h0 = histogram[2 * t], h1 = histogram[2 * t + 1];
+        int h0 = 0, h1 = 0;
+#pragma unroll
+        for (int i = 0; i < SELECT_COPIES; ++i) {
+            h0 += histogram[i][2 * t];
+            h1 += histogram[i][2 * t + 1];
+        }
         int above = h0 + h1;
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {

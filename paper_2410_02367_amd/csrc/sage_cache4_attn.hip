@@ -304,12 +304,75 @@ __device__ __forceinline__ void wave_order() {       // LDS written by other lan
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 }
+__device__ __forceinline__ void store4(void* out, long at, int type, c4f x) {
+    if (type == TYPE_F16) {
+        typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+        *(h4*)((_Float16*)out + at) = __builtin_convertvector(x, h4);
+    } else {
+        typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+        *(b4*)((__bf16*)out + at) = __builtin_convertvector(x, b4);
+    }
+}
 __device__ __forceinline__ float over_h(float x, bool sum) {
     const float y = __shfl_xor(x, 16, 64);
     x = sum ? x + y : __builtin_fmaxf(x, y);
     const float z = __shfl_xor(x, 32, 64);
     return sum ? x + z : __builtin_fmaxf(x, z);
 }
+}  // namespace
+
+namespace {
+// Which (sequence, head), tile of rows and chunk of keys a workgroup has: slabs dealt out to the XCDs, so that the workgroups of one
+// share its keys in one L2; the tiles that see most first.
+struct RowsPlace {
+    int slab, tile, split, slabs;
+    __device__ __forceinline__ RowsPlace(const Cache4& c, const CacheQueries& q, int tiles, int n_splits) {
+        slabs = q.B * c.heads;
+        const int per_slab = tiles * n_splits;
+        int rest;
+        if (slabs % 8 == 0) {
+            const int i = blockIdx.x >> 3;
+            slab = (i / per_slab) * 8 + (blockIdx.x & 7);
+            rest = i % per_slab;
+        } else {
+            slab = blockIdx.x / per_slab;
+            rest = blockIdx.x % per_slab;
+        }
+        split = rest % n_splits;
+        tile = tiles - 1 - rest / n_splits;
+    }
+};
+// Where a row's result goes: the output, or the partial results of a chunk, [chunk][slab][row][D] normalized fp32 and the base-2
+// logarithm of their sums.
+struct RowResult {
+    float norm, log_sum;
+    size_t part_row, lse_at;
+    long b, hq;
+    int tq;
+    // live: the row is there; M, total: reference and sum of its weights
+    __device__ __forceinline__ RowResult(const RowsPlace& at, const CacheQueries& q, int head, int share, int row, bool live, float M, float total,
+                                         int all_rows) {
+        live = live && total != 0.0f;
+        norm = live ? 1.0f / total : 0.0f;
+        log_sum = live ? M + __builtin_amdgcn_logf(total) : -__builtin_inff();
+        part_row = ((size_t)at.split * at.slabs + at.slab) * all_rows + row;
+        tq = row / share;
+        b = at.slab / (q.Hq / share);
+        hq = head * share + row - tq * share;
+        lse_at = ((size_t)b * q.Hq + hq) * q.Nq + tq;
+    }
+    __device__ __forceinline__ void put_sum(const CacheQueries& q, float* lse, float* part_lse, bool partial) const {
+        if (partial) part_lse[part_row] = log_sum;
+        else if (lse != nullptr) lse[lse_at] = log_sum * LN2;
+    }
+    // channels d .. d + 3
+    template <int D>
+    __device__ __forceinline__ void put(const CacheQueries& q, void* out, const RowStrides& os, float* part, c4f x, int d) const {
+        x = norm == 0.0f ? (c4f){0.0f, 0.0f, 0.0f, 0.0f} : x * norm;
+        if (part != nullptr) *(c4f*)(part + part_row * D + d) = x;
+        else store4(out, b * os.b + hq * os.h + tq * os.n + d, q.type, x);
+    }
+};
 }  // namespace
 
 // grid: (tile of rows, chunk of keys, (sequence, head)) from one index.  part != nullptr: partial results, [chunk][slab][row][D]
@@ -324,25 +387,14 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
     __shared__ __attribute__((aligned(16))) unsigned char lds[MERGE > STAGE ? MERGE : STAGE];
     __shared__ float s_m[WAVES][16], s_l[WAVES][16];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
-    const int slabs = q.B * c.heads, per_slab = tiles * n_splits;
-    // slabs dealt out to the XCDs, so that the workgroups of one share its keys in one L2
-    int slab, rest;
-    if (slabs % 8 == 0) {
-        const int i = blockIdx.x >> 3;
-        slab = (i / per_slab) * 8 + (blockIdx.x & 7);
-        rest = i % per_slab;
-    } else {
-        slab = blockIdx.x / per_slab;
-        rest = blockIdx.x % per_slab;
-    }
-    const int split = rest % n_splits;
-    const int b = slab / c.heads, head = slab - b * c.heads, share = q.Hq / c.heads;
+    const RowsPlace at(c, q, tiles, n_splits);
+    const int b = at.slab / c.heads, head = at.slab - b * c.heads, share = q.Hq / c.heads;
     const RowRange range(c, q, b, share);
-    const int row0 = (tiles - 1 - rest / n_splits) * 16 * QT, all_rows = q.Nq * share;
+    const int row0 = at.tile * 16 * QT, all_rows = q.Nq * share;
     const int there = min(range.rows - row0, 16 * QT);               // rows of this workgroup that are there
     const int first_end = there > 0 ? range.end(row0 / share, q.causal) : 0;
     const int last_end = there > 0 ? range.end((row0 + there - 1) / share, q.causal) : 0;
-    const int k_begin = split * chunk, k_end = min(k_begin + chunk, last_end);
+    const int k_begin = at.split * chunk, k_end = min(k_begin + chunk, last_end);
     if (part != nullptr && k_begin >= last_end) return;              // (the merge knows)
 
     Queries4<D> query[QT];
@@ -480,36 +532,269 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
         __syncthreads();
         const int row = row0 + 16 * i + col;
         if (row >= all_rows) continue;
-        const bool live = row < range.rows;
-        const float norm = live && total != 0.0f ? 1.0f / total : 0.0f;
-        const float log_sum = live && total != 0.0f ? top + __builtin_amdgcn_logf(total) : -__builtin_inff();
-        const int tq = row / share, g = row - tq * share;
-        const size_t prow = ((size_t)split * slabs + slab) * all_rows + row;
-        if (wave == 0 && h == 0) {
-            if (part != nullptr) part_lse[prow] = log_sum;
-            else if (lse != nullptr) lse[((size_t)b * q.Hq + head * share + g) * q.Nq + tq] = log_sum * LN2;
-        }
+        const RowResult r(at, q, head, share, row, row < range.rows, top, total, all_rows);
+        if (wave == 0 && h == 0) r.put_sum(q, lse, part_lse, part != nullptr);
 #pragma unroll
         for (int n = 0; n < CT / WAVES; ++n) {
             const int ct = wave + WAVES * n;
             c4f x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) x += *(const c4f*)(lds + ((w * CT + ct) * 64 + lane) * 16);
-            x = norm == 0.0f ? (c4f){0.0f, 0.0f, 0.0f, 0.0f} : x * norm;
-            const int d = 16 * ct + 4 * h;
-            if (part != nullptr) {
-                *(c4f*)(part + prow * D + d) = x;
+            r.template put<D>(q, out, os, part, x, 16 * ct + 4 * h);
+        }
+    }
+}
+
+// ---- many rows: operands made once for all of a workgroup's wavefronts
+namespace {
+// A wavefront's share of a tile of 64 keys, as it comes from memory: K's words of piece `wave`, a quarter of every V row, the
+// scales (wavefront 0: K's, 1: V's; a key per lane).
+template <int D, int NG>
+struct TileShare {
+    typedef typename ScaleWord<NG>::type scale_t;
+    typedef unsigned words __attribute__((ext_vector_type(D / 32)));
+    static constexpr int ROW = D / 2;
+    words k, v;
+    scale_t scale;
+    unsigned bad;
+    __device__ __forceinline__ void request(const Cache4& c, const unsigned char* head, const PageIds& pages, int k0, int lane, int wave) {
+        const int col = lane & 15, h = lane >> 4, mask = c.page() - 1;
+        const unsigned char *piece, *mine;          // the blocks of piece `wave` and of the lane's key
+        int piece_row, row;
+        if (c.shift >= 6) {
+            bool ok;
+            piece = mine = KeyTile<D, NG, true>::block(c, head, pages.id[0], ok);
+            bad = ok ? 0u : 15u;
+            piece_row = (k0 & mask) + 16 * wave;
+            row = (k0 & mask) + lane;
+        } else {
+            const unsigned char* at[4];
+            bad = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                bool ok;
+                at[j] = KeyTile<D, NG, true>::block(c, head, pages.id[j], ok);
+                if (!ok) bad |= 1u << j;
+            }
+            piece = mine = at[0];
+#pragma unroll
+            for (int j = 1; j < 4; ++j) {
+                piece = wave == j ? at[j] : piece;
+                mine = h == j ? at[j] : mine;
+            }
+            piece_row = (k0 + 16 * wave) & mask;
+            row = (k0 + lane) & mask;
+        }
+        k = *(const words*)(piece + (piece_row + col) * ROW + h * (D / 8));
+        v = *(const words*)(mine + (ROW << c.shift) + row * ROW + wave * (ROW / 4));
+        if (wave < 2) scale = *(const scale_t*)(mine + ((D + 2 * NG * wave) << c.shift) + row * 2 * NG);
+    }
+};
+// A tile as operands: [piece][step] of K, [half][channels of 16] of V, 16 bytes per lane each; the scales.
+template <int D, int NG>
+struct TileStage {
+    half8 k[4][D / 32][64], v[2][D / 16][64];
+    _Float16 ks[TILE * NG], vs[TILE * NG];
+};
+}  // namespace
+
+// 128 rows per workgroup, 32 per wavefront; the wavefronts walk the tiles together.  Each makes a quarter of a tile's operands
+// in LDS, one tile ahead, in two buffers, a barrier per tile.  The 18 vector instructions that a word of K and a word of V cost are
+// spent once for 128 rows instead of once for 32; the price is the LDS, 128 KB read per tile and 128 rows.
+template <int D, int NG>
+__global__ void __launch_bounds__(WAVES * 64, 2)
+cache4_attn_rows_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides os, float* __restrict__ lse, float* __restrict__ part,
+                        float* __restrict__ part_lse, int tiles, int n_splits, int chunk) {
+    constexpr int QT = 2, CT = D / 16, STEPS = D / 32 / NG, RAW = TILE * D / 8;
+    __shared__ TileStage<D, NG> stage[2];
+    __shared__ __attribute__((aligned(16))) unsigned char raw_v[WAVES][RAW];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
+    const RowsPlace at(c, q, tiles, n_splits);
+    const int b = at.slab / c.heads, head = at.slab - b * c.heads, share = q.Hq / c.heads;
+    const RowRange range(c, q, b, share);
+    const int all_rows = q.Nq * share, group0 = at.tile * WAVES * 16 * QT, row0 = group0 + wave * 16 * QT;
+    // what the wavefront's first and last rows see, and the workgroup's last
+    const int there = min(range.rows - row0, 16 * QT), last_there = min(range.rows - group0, WAVES * 16 * QT);
+    const int first_end = there > 0 ? range.end(row0 / share, q.causal) : 0;
+    const int wave_end = there > 0 ? range.end((row0 + there - 1) / share, q.causal) : 0;
+    const int last_end = last_there > 0 ? range.end((group0 + last_there - 1) / share, q.causal) : 0;
+    const int k_begin = at.split * chunk, k_end = min(k_begin + chunk, last_end);
+    if (part != nullptr && k_begin >= last_end) return;              // (the merge knows)
+
+    Queries4<D> query[QT];
+    float sc[QT], M[QT], l[QT];
+    int end[QT];
+    c4f o[QT][CT];
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        const int row = min(row0 + 16 * i + col, max(range.rows - 1, 0)), tq = row / share, g = row - tq * share;
+        sc[i] = query[i].load(q, b * q.strides.b + (head * share + g) * q.strides.h + tq * q.strides.n, h);
+        end[i] = range.end(tq, q.causal);
+        M[i] = UNSET;
+        l[i] = 0.0f;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) o[i][ct] = (c4f){0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    const int* const table = c.table + (size_t)b * c.columns;
+    const unsigned char* const head_at = c.data + head * c.block_bytes();
+    TileShare<D, NG> own;
+    PageIds pages;
+    // the share that has arrived, the tile from k0 on, into a buffer
+    auto put = [&](TileStage<D, NG>& to, int k0) {
+        typedef typename TileShare<D, NG>::words words;
+        typedef typename TileShare<D, NG>::scale_t scale_t;
+        wave_order();
+        *(words*)(raw_v[wave] + lane * (D / 8)) = own.v;
+        if (wave < 2) {
+            // (a row past the last key holds anything, its scale is no number perhaps: 0 instead)
+            const bool absent = k0 + lane >= last_end || (own.bad >> h & 1);
+            *(scale_t*)((wave == 0 ? to.ks : to.vs) + lane * NG) = absent ? (scale_t)(0) : own.scale;
+        }
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) to.k[wave][i][lane] = operand(own.k[i]);
+        wave_order();
+        // V transposed: lane's channel, nibble i of the words: key 16 (i / 4) + 4 h + i % 4
+        const int v_key = 16 * (col >> 2) + 4 * h + (col & 3);
+#pragma unroll
+        for (int n = 0; n < D / 64; ++n) {
+            const c2i x = __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) c2i*)(raw_v[wave] + v_key * (D / 8) + 8 * n));
+            to.v[0][D / 64 * wave + n][lane] = operand((unsigned)x[0]);
+            to.v[1][D / 64 * wave + n][lane] = operand((unsigned)x[1]);
+        }
+    };
+    unsigned bad = 0;
+    if (k_begin < k_end) {
+        pages.look_up(c, table, k_begin);
+        own.request(c, head_at, pages, k_begin, lane, wave);
+        pages.look_up(c, table, k_begin + TILE);
+        put(stage[0], k_begin);
+        bad = own.bad;
+        if (k_begin + TILE < k_end) {
+            own.request(c, head_at, pages, k_begin + TILE, lane, wave);
+            pages.look_up(c, table, k_begin + 2 * TILE);
+        }
+    }
+    __syncthreads();
+    typedef unsigned scales_t __attribute__((ext_vector_type(2 * NG)));
+    struct Half {               // 32 keys: scores, V's scales, weights
+        float s[QT][2][4];
+        scales_t vs[2];
+        half8 w[QT][NG];
+        float sum[QT];
+    };
+    auto score = [&](Half& x, const TileStage<D, NG>& now, int u) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const scales_t ks = *(const scales_t*)(now.ks + (16 * (2 * u + j) + 4 * h) * NG);
+            x.vs[j] = *(const scales_t*)(now.vs + (16 * (2 * u + j) + 4 * h) * NG);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                c4f a[QT];
+#pragma unroll
+                for (int n = 0; n < STEPS; ++n) {
+                    const half8 k = now.k[2 * u + j][g * STEPS + n][lane];
+#pragma unroll
+                    for (int i = 0; i < QT; ++i)
+                        a[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, query[i].op[g * STEPS + n], n == 0 ? (c4f){0.0f, 0.0f, 0.0f, 0.0f} : a[i], 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < QT; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float scale = (float)half_of(ks[(r * NG + g) / 2], (r * NG + g) & 1);
+                        x.s[i][j][r] = __builtin_fmaf(scale, a[i][r], g == 0 ? 0.0f : x.s[i][j][r]);
+                    }
+            }
+        }
+    };
+    auto hide = [&](Half& x, int k0, int u) {
+#pragma unroll
+        for (int i = 0; i < QT; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int last = bad >> (2 * u + j) & 1 ? 0 : end[i];
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (k0 + 16 * (2 * u + j) + 4 * h + r >= last) x.s[i][j][r] = -__builtin_inff();
+            }
+    };
+    auto weighed = [&](Half& x) {
+        bool low = false;
+#pragma unroll
+        for (int i = 0; i < QT; ++i) low |= weigh<NG>(x.s[i], sc[i], M[i], x.vs, x.w[i], x.sum[i]);
+        return low;
+    };
+    auto raise = [&](Half& x) {
+#pragma unroll
+        for (int i = 0; i < QT; ++i) {
+            const float M_new = __builtin_fmaxf(M[i], over_h(reference<NG>(x.s[i], sc[i], x.vs), false));
+            const float alpha = __builtin_amdgcn_exp2f(M[i] - M_new);
+            M[i] = M_new;
+            l[i] *= alpha;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) o[i][ct] *= alpha;
+            weigh<NG>(x.s[i], sc[i], M[i], x.vs, x.w[i], x.sum[i]);
+        }
+    };
+    auto values = [&](const Half& x, const TileStage<D, NG>& now, int u) {
+#pragma unroll
+        for (int i = 0; i < QT; ++i) l[i] += x.sum[i];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            const half8 v = now.v[u][ct][lane];
+#pragma unroll
+            for (int i = 0; i < QT; ++i) o[i][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, x.w[i][ct * NG / CT], o[i][ct], 0, 0, 0);
+        }
+    };
+    for (int k0 = k_begin, turn = 0; k0 < k_end; k0 += TILE, turn ^= 1) {
+        const TileStage<D, NG>& now = stage[turn];
+        const unsigned now_bad = bad;
+        const bool more = k0 + TILE < k_end;
+        if (k0 < wave_end) {
+            // products of one half beside the other half's weights
+            const bool masked = k0 + TILE > first_end || now_bad != 0;
+            if constexpr (NG <= 2) {
+                Half x, y;
+                score(x, now, 0);
+                if (masked) hide(x, k0, 0);
+                score(y, now, 1);
+                if (__builtin_expect(weighed(x), 0)) raise(x);
+                if (masked) hide(y, k0, 1);
+                values(x, now, 0);
+                if (__builtin_expect(weighed(y), 0)) raise(y);
+                values(y, now, 1);
             } else {
-                const long at = b * os.b + (head * share + g) * os.h + tq * os.n + d;
-                if (q.type == TYPE_F16) {
-                    typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-                    *(h4*)((_Float16*)out + at) = __builtin_convertvector(x, h4);
-                } else {
-                    typedef __bf16 b4 __attribute__((ext_vector_type(4)));
-                    *(b4*)((__bf16*)out + at) = __builtin_convertvector(x, b4);
+                // (four groups' operands and scales: no registers for two halves)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    Half x;
+                    score(x, now, u);
+                    if (masked) hide(x, k0, u);
+                    if (__builtin_expect(weighed(x), 0)) raise(x);
+                    values(x, now, u);
                 }
             }
         }
+        if (more) {
+            put(stage[turn ^ 1], k0 + TILE);
+            bad = own.bad;
+            if (k0 + 2 * TILE < k_end) {
+                own.request(c, head_at, pages, k0 + 2 * TILE, lane, wave);
+                pages.look_up(c, table, k0 + 3 * TILE);
+            }
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        const float total = over_h(l[i], true);
+        const int row = row0 + 16 * i + col;
+        if (row >= all_rows) continue;
+        const RowResult r(at, q, head, share, row, row < range.rows, M[i], total, all_rows);
+        if (h == 0) r.put_sum(q, lse, part_lse, part != nullptr);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) r.template put<D>(q, out, os, part, o[i][ct], 16 * ct + 4 * h);
     }
 }
 
@@ -583,14 +868,7 @@ __global__ void __launch_bounds__(256) cache4_merge_kernel(Cache4 c, CacheQuerie
     if (total != 0.0f) x *= 1.0f / total;
     if (d == 0 && lse != nullptr)
         lse[((size_t)b * q.Hq + head * share + g) * q.Nq + tq] = total != 0.0f ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
-    const long at = b * os.b + (head * share + g) * os.h + tq * os.n + d;
-    if (q.type == TYPE_F16) {
-        typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-        *(h4*)((_Float16*)out + at) = __builtin_convertvector(x, h4);
-    } else {
-        typedef __bf16 b4 __attribute__((ext_vector_type(4)));
-        *(b4*)((__bf16*)out + at) = __builtin_convertvector(x, b4);
-    }
+    store4(out, b * os.b + (head * share + g) * os.h + tq * os.n + d, q.type, x);
 }
 
 // ---- the weights of the keys
@@ -641,8 +919,18 @@ __device__ __forceinline__ void add_weights(float (&sum)[4][4], const KeyOperand
         }
     }
 }
+// What the 64 slots from k0 on had: lane (col < 4, h) those of keys 16 col + 4 h ..  Requested with the keys, a tile ahead: a load
+// behind the next tile's would be waited for together with it.
+struct Had {
+    float x[4];
+    __device__ __forceinline__ void request(const float* had, int k0, int width, int lane) {
+        const int key = k0 + 16 * (lane & 15) + 4 * (lane >> 4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = had != nullptr && (lane & 15) < 4 && key + r < width ? had[key + r] : 0.0f;
+    }
+};
 // adds up the columns and writes the 64 sums
-__device__ __forceinline__ void put_weights(float (&sum)[4][4], unsigned bad, const float* had, float* out, int k0, int width, int lane) {
+__device__ __forceinline__ void put_weights(float (&sum)[4][4], unsigned bad, const Had& had, float* out, int k0, int width, int lane) {
     const int col = lane & 15, h = lane >> 4;
     float mine[4] = {};
 #pragma unroll
@@ -652,12 +940,11 @@ __device__ __forceinline__ void put_weights(float (&sum)[4][4], unsigned bad, co
             const float x = over_columns(sum[j][r]);
             mine[r] = col == j ? x : mine[r];
         }
-    // lanes col < 4: keys 16 col + 4 h ..
     if (col >= 4) return;
     const int key = k0 + 16 * col + 4 * h;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-        if (key + r < width) out[key + r] = (had != nullptr ? had[key + r] : 0.0f) + (bad >> col & 1 ? 0.0f : mine[r]);
+        if (key + r < width) out[key + r] = had.x[r] + (bad >> col & 1 ? 0.0f : mine[r]);
 }
 }  // namespace
 
@@ -677,11 +964,13 @@ __global__ void __launch_bounds__(WAVES * 64) cache4_weights_few_kernel(Cache4 c
     int k0 = blockIdx.x * chunk + TILE * wave;
     typedef KeyTile<D, NG, false> Tile;
     Tile tile;
+    Had next_had;
     PageIds pages;
     const int* const table = c.table + (size_t)b * c.columns;
     const unsigned char* const head_at = c.data + head * c.block_bytes();
     if (k0 < seen) {
         pages.look_up(c, table, k0);
+        next_had.request(had, k0, width, lane);
         tile.request(c, head_at, pages, k0, lane);
         pages.look_up(c, table, k0 + NEXT);
         const int row = min(col, range.rows - 1), tq = row / share, g = row - tq * share;
@@ -698,13 +987,15 @@ __global__ void __launch_bounds__(WAVES * 64) cache4_weights_few_kernel(Cache4 c
             KeyOperands<D, NG> keys;
             keys.make(tile, s_ks[wave], h);
             const unsigned bad = tile.bad;
+            const Had now_had = next_had;
             if (k0 + NEXT < seen) {
+                next_had.request(had, k0 + NEXT, width, lane);
                 tile.request(c, head_at, pages, k0 + NEXT, lane);
                 pages.look_up(c, table, k0 + 2 * NEXT);
             }
             float sum[4][4] = {};
             add_weights<D, NG>(sum, keys, query.op, sc, reference, end - k0, k0 + TILE <= first_end, h);
-            put_weights(sum, bad, had, to, k0, width, lane);
+            put_weights(sum, bad, now_had, to, k0, width, lane);
         }
     }
     // slots that no query sees keep what they had
@@ -732,6 +1023,8 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache4_weights_kernel(Cache4 c,
     const int k_first = blockIdx.x * WAVES * TILE, k0 = k_first + wave * TILE;
     float sum[4][4] = {};
     unsigned bad = 0;
+    Had its_had;
+    its_had.request(had, k0, width, lane);
     if (k_first < last_end) {                   // (the same for the whole workgroup)
         KeyOperands<D, NG> keys;
         {
@@ -773,31 +1066,38 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache4_weights_kernel(Cache4 c,
             }
         }
     }
-    if (k0 < width) put_weights(sum, bad, had, to, k0, width, lane);
+    if (k0 < width) put_weights(sum, bad, its_had, to, k0, width, lane);
 }
 
 namespace {
-// How a call is cut.  Rows: 16 or 32 per workgroup.  (64, with one wavefront per SIMD: 64 rows of 64 slabs of 16K keys 95 us, two
-// workgroups of 32 rows 90; 4096 rows of 8 slabs of 8K 233 / 216.)  Keys: chunks of a multiple of 256, as many as it takes to have
-// WANTED workgroups, two per compute unit (us with 256 / 512 / 1024 workgroups: 256 slabs of 16K keys 146 / 112 / 110, 8 of 128K 40 / 36 /
-// 40, 64 of 16K with 64 rows 110 / 90 / 98), none shorter than 512 unless the caller asks for it.
+// How a call is cut.  Keys: chunks of a multiple of 256, as many as it takes to have WANTED workgroups, two per compute unit (us with
+// 256 / 512 / 1024 workgroups: 256 slabs of 16K keys 146 / 112 / 110, 8 of 128K 40 / 36 / 40, 64 of 16K with 64 rows 110 / 90 / 98), none
+// shorter than 512 unless the caller asks for it.  Rows: 16 or 32 per workgroup, whose wavefronts share the keys; or 128, whose
+// wavefronts share the operands, where there are that many and the chunks are long (us with 32 / 128: 4096 rows of 8 slabs of 32K
+// keys 1117 / 934, of 4K 117 / 111, 128 rows of 64 slabs of 16K 125 / 108; chunks of 512 keys: 512 rows of 32 slabs of 2K 42 / 49).
 struct AttnPlan {
-    int qt, tiles, n_splits, chunk;
+    int rows, tiles, n_splits, chunk;       // rows of a workgroup
 };
-constexpr int WANTED = 512, WANTED_FEW = 1024;
+constexpr int WANTED = 512, WANTED_FEW = 1024, MANY_ROWS = 128, LONG_CHUNK = 2048;
 AttnPlan plan(int B, int Hq, int Hkv, int Nq, int capacity, int requested) {
     const int rows = Hq / Hkv * Nq;
-    AttnPlan p;
-    p.qt = rows <= 16 ? 1 : 2;
-    p.tiles = (rows + 16 * p.qt - 1) / (16 * p.qt);
-    const long groups = (long)B * Hkv * p.tiles;
-    long n = requested > 0 ? requested : WANTED / groups;
-    const int least = requested > 0 ? 256 : 512;
-    if (n > capacity / least) n = capacity / least;
-    if (n < 1) n = 1;
-    p.chunk = (int)(((capacity + n - 1) / n + 255) / 256 * 256);
-    p.n_splits = (capacity + p.chunk - 1) / p.chunk;
-    return p;
+    auto cut = [&](int per) {
+        AttnPlan p;
+        p.rows = per;
+        p.tiles = (rows + per - 1) / per;
+        long n = requested > 0 ? requested : WANTED / ((long)B * Hkv * p.tiles);
+        const int least = requested > 0 ? 256 : 512;
+        if (n > capacity / least) n = capacity / least;
+        if (n < 1) n = 1;
+        p.chunk = (int)(((capacity + n - 1) / n + 255) / 256 * 256);
+        p.n_splits = (capacity + p.chunk - 1) / p.chunk;
+        return p;
+    };
+    if (rows > 96) {
+        const AttnPlan p = cut(MANY_ROWS);
+        if (p.chunk >= LONG_CHUNK) return p;
+    }
+    return cut(rows <= 16 ? 16 : 32);
 }
 }  // namespace
 
@@ -811,8 +1111,9 @@ static void launch_attn_form(const AttnPlan& p, const Cache4& c, const CacheQuer
                              float* part_lse, hipStream_t st) {
     const unsigned grid = (unsigned)(q.B * c.heads * p.tiles * p.n_splits);
 #define SAGE_CACHE4_ATTN(QT) cache4_attn_kernel<D, NG, QT><<<grid, WAVES * 64, 0, st>>>(c, q, out, os, lse, part, part_lse, p.tiles, p.n_splits, p.chunk)
-    if (p.qt == 1) SAGE_CACHE4_ATTN(1);
-    else SAGE_CACHE4_ATTN(2);
+    if (p.rows == 16) SAGE_CACHE4_ATTN(1);
+    else if (p.rows == 32) SAGE_CACHE4_ATTN(2);
+    else cache4_attn_rows_kernel<D, NG><<<grid, WAVES * 64, 0, st>>>(c, q, out, os, lse, part, part_lse, p.tiles, p.n_splits, p.chunk);
 #undef SAGE_CACHE4_ATTN
 }
 

@@ -83,6 +83,23 @@ def test_keys_shared_by_workgroups(n_splits, Nq):
     case(7, 2, 4, 1, Nq, 128, 64, 32, "f16", [1100, 130], n_splits=n_splits)
 
 
+# a table with room for 2048 tokens and more: with one chunk, the form for many rows
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("D,group,page", FORMS)
+@pytest.mark.parametrize("Hq,Hkv,Nq,lengths,count", [(1, 1, 97, [97, 300], None), (8, 2, 33, [200, 20], None), (4, 1, 70, [70, 333], [70, 3]),
+                                                     (6, 2, 128, [1, 129], [128, 128])])
+def test_many_rows(Hq, Hkv, Nq, lengths, count, D, group, page, kind):
+    case(Nq + page, 2, Hq, Hkv, Nq, D, page, group, kind, lengths, count, extra=2048 // page, n_splits=1, weights=False)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_rows_pages_that_are_none_and_several_chunks(causal):
+    case(21, 2, 2, 1, 60, 64, 16, 32, "f16", [150, 64], bad=[(0, 0), (0, 4), (1, 3), (1, 2)], extra=128, n_splits=1, causal=causal, weights=False)
+    case(22, 1, 2, 1, 49, 128, 64, 32, "f16", [2700], extra=24, n_splits=2, causal=causal, weights=False)
+    case(23, 1, 1, 1, 130, 128, 64, 64, "f16", [4200], q_gain=25.0, n_splits=2, causal=causal, weights=False)
+    case(24, 2, 4, 2, 80, 64, 16, 64, "bf16", [90, 85], extra=128, n_splits=1, q_gain=25.0, causal=causal, weights=False)
+
+
 def test_lengths_beyond_the_table_and_below_zero():
     case(8, 3, 2, 2, 3, 64, 16, 64, "f16", [40, 7, 33], count=[5, -1, 3])
     import paper_2410_02367_amd as sage
