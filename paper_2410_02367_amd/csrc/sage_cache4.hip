@@ -107,18 +107,22 @@ __global__ void __launch_bounds__(256) cache4_append_kernel(Cache4 c, const void
     const int there = count != nullptr ? min(count[b], N) : N;
     // (a row's threads stay or leave together: group_max looks at no other row's)
     if (n >= there) return;
+    // the rows are on their way while the page is looked up
+    float x[8], y[8];
+    row8<TYPE>(k, b * ks.b + h * ks.h + n * ks.n + 8 * o, x);
+    row8<TYPE>(v, b * vs.b + h * vs.h + n * vs.n + 8 * o, y);
+    float mean[8] = {};
+    if (k_mean != nullptr) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mean[e] = k_mean[(size_t)bh * D + 8 * o + e];
+    }
     const long slot = (long)start[b] + n;
     if (slot < 0 || slot >= c.capacity()) return;
     unsigned char* block = c.block(b, h, (int)slot);
     if (block == nullptr) return;
     const int r = (int)slot & (c.page() - 1);
-    float x[8], y[8];
-    row8<TYPE>(k, b * ks.b + h * ks.h + n * ks.n + 8 * o, x);
-    row8<TYPE>(v, b * vs.b + h * vs.h + n * vs.n + 8 * o, y);
-    if (k_mean != nullptr) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] -= k_mean[(size_t)bh * D + 8 * o + e];
-    }
+    for (int e = 0; e < 8; ++e) x[e] -= mean[e];
     numbers(x);
     numbers(y);
     const _Float16 dk = scale_of(group_max<GROUP>(x)), dv = scale_of(group_max<GROUP>(y));
@@ -205,7 +209,7 @@ __global__ void __launch_bounds__(SELECT_NT) cache4_select_kernel(const int* __r
                                                                   int* __restrict__ out_lengths, int keep, int recent) {
     // (copies, one for every fourth lane: weights of like size fall into few bins, and additions to one word wait for each other)
     __shared__ int histogram[SELECT_COPIES][SELECT_BINS + 8];
-    __shared__ int s_digit, s_above, s_total[SELECT_WAVES], s_gt[SELECT_WAVES], s_eq[SELECT_WAVES];
+    __shared__ int s_digit, s_above, s_count, s_total[SELECT_WAVES], s_gt[SELECT_WAVES], s_eq[SELECT_WAVES];
     const int bh = blockIdx.x, b = bh / heads, t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int n = min(max(lengths[b], 0), capacity);
     int* const to = kept + (size_t)bh * keep;
@@ -281,14 +285,20 @@ __global__ void __launch_bounds__(SELECT_NT) cache4_select_kernel(const int* __r
         if (above < left && left <= above + h1) {
             s_digit = 2 * t + 1;
             s_above = above;
+            s_count = h1;
         } else if (above + h1 < left && left <= above + h1 + h0) {
             s_digit = 2 * t;
             s_above = above + h1;
+            s_count = h0;
         }
         __syncthreads();
         found |= (unsigned)s_digit << shift;
         mask |= bins << shift;
         left -= s_above;
+        if (left == s_count) {          // all keys with these bits stay: whatever the others are, from 0 on
+            left = m;
+            break;
+        }
     }
     int gt = 0, eq = 0;
     walk([&](unsigned u, int, bool is) {

@@ -35,7 +35,7 @@ constexpr float UNSET = -1e30f;             // a reference below every score: th
 constexpr _Float16 W_LIMIT = 4096.0f;
 constexpr float P_LIMIT = 0x1p45f;
 constexpr float RAISE = 4.0f, SMALLEST = 0x1p-36f;
-constexpr int TILE = 64, WAVES = 4;
+constexpr int TILE = 64, WAVES = 4, FEW_CHUNK = 2048;
 
 // 8 codes of a word -> operand registers: element 2 m + s is the code of nibble m + 4 s, times 16 where m is odd.  A nibble in the
 // low mantissa bits of 1024 is 1024 + nibble (or + 16 nibble); the packed subtraction is exact and leaves a small whole number.
@@ -224,22 +224,6 @@ __device__ __forceinline__ unsigned max3_pairs(unsigned a, unsigned b, unsigned 
     return d;
 }
 __device__ __forceinline__ _Float16 half_of(unsigned w, int hi) { return __builtin_bit_cast(_Float16, (unsigned short)(hi ? w >> 16 : w)); }
-
-// scores of 16 keys and 16 rows, scaled by K's scales: register r is key 4 h + r
-template <int D, int NG>
-__device__ __forceinline__ c4f scores(const half8 (&k)[D / 32], const half8 (&q)[D / 32], const unsigned (&ks)[2 * NG]) {
-    constexpr int STEPS = D / 32 / NG;
-    c4f s;
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-        c4f a = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) a = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[g * STEPS + i], q[g * STEPS + i], a, 0, 0, 0);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[r] = __builtin_fmaf((float)half_of(ks[(r * NG + g) / 2], (r * NG + g) & 1), a[r], g == 0 ? 0.0f : s[r]);
-    }
-    return s;
-}
 
 // The weights of 32 keys for 16 rows: register r of the two score tiles is keys 4 h + r and 16 + 4 h + r, element 2 r and 2 r + 1
 // of an operand; those of odd r meet 16-fold codes and are 2^-4 of the others.  -> whether the reference is too low.
@@ -872,137 +856,134 @@ __global__ void __launch_bounds__(256) cache4_merge_kernel(Cache4 c, CacheQuerie
 }
 
 // ---- the weights of the keys
+// The products are turned round: rows of queries times columns of keys, so that a key's sum runs over a lane's registers and the
+// four lanes of a column (over 16 columns of rows: 192 vector instructions per tile, here 28).
 namespace {
-// the sum over the 16 columns of rows, in all of them
-__device__ __forceinline__ float over_columns(float x) {
-    auto rotated = [](float y, auto CTRL) {
-        const int v = __builtin_bit_cast(int, y);
-        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(v, v, decltype(CTRL)::value, 0xF, 0xF, false));
-    };
-    x += rotated(x, std::integral_constant<int, 0x128>{});
-    x += rotated(x, std::integral_constant<int, 0x124>{});
-    x += rotated(x, std::integral_constant<int, 0x122>{});
-    return x + rotated(x, std::integral_constant<int, 0x121>{});
-}
 // a row's lse as the base-2 reference its weights are relative to; of a row that saw nothing one that leaves no weight
 __device__ __forceinline__ float row_reference(float lse) { return lse == -__builtin_inff() ? __builtin_inff() : lse * LOG2E; }
 
-// the words and scales of 64 keys as operands
-template <int D, int NG>
-struct KeyOperands {
-    half8 k[4][D / 32];
-    unsigned ks[4][2 * NG];
-    // `staged`: the scales of the wavefront's keys, [key][group]
-    __device__ __forceinline__ void make(const KeyTile<D, NG, false>& tile, const _Float16* staged, int h) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            typedef unsigned scales_t __attribute__((ext_vector_type(2 * NG)));
-            const scales_t a = *(const scales_t*)(staged + (16 * j + 4 * h) * NG);
-#pragma unroll
-            for (int e = 0; e < 2 * NG; ++e) ks[j][e] = a[e];
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) k[j][i] = operand(tile.k[j][i]);
-        }
-    }
+// what the rows 4 h + r of a lane need: scale of the exponent, reference, slots seen
+struct LaneRows {
+    float sc[4], reference[4];
+    int end[4];
 };
-// sum[j][r] += the weights that 16 rows give to key 16 j + 4 h + r of a tile; end: slots that the lane's row sees, from k0 on
+template <int NG> using LaneScales = unsigned[(NG + 1) / 2];
+// -> the weights that 16 rows give to the lane's key, rows 4 h .. 4 h + 3 of them; key: the slot.  whole: every row sees it
 template <int D, int NG>
-__device__ __forceinline__ void add_weights(float (&sum)[4][4], const KeyOperands<D, NG>& keys, const half8 (&q)[D / 32], float sc, float reference,
-                                            int end, bool whole, int h) {
+__device__ __forceinline__ float piece_weights(const half8 (&q)[D / 32], const half8 (&k)[D / 32], const LaneScales<NG>& ks, const LaneRows& rows, int key,
+                                               bool whole) {
+    constexpr int STEPS = D / 32 / NG;
+    c4f s;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const c4f s = scores<D, NG>(keys.k[j], q, keys.ks[j]);
+    for (int g = 0; g < NG; ++g) {
+        c4f a = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, -reference));
-            sum[j][r] += whole || 16 * j + 4 * h + r < end ? p : 0.0f;
-        }
+        for (int i = 0; i < STEPS; ++i) a = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[g * STEPS + i], k[g * STEPS + i], a, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[r] = __builtin_fmaf((float)half_of(ks[g / 2], g & 1), a[r], g == 0 ? 0.0f : s[r]);
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], rows.sc[r], -rows.reference[r]));
+        sum += whole || key < rows.end[r] ? p : 0.0f;
+    }
+    return sum;
+}
+// the scales of a key, staged as [key][group]
+template <int NG>
+__device__ __forceinline__ void lane_scales(const _Float16* staged, int key, LaneScales<NG>& ks) {
+    const typename ScaleWord<NG>::type w = *(const typename ScaleWord<NG>::type*)(staged + key * NG);
+    if constexpr (NG == 4) {
+        ks[0] = w[0];
+        ks[1] = w[1];
+    } else {
+        ks[0] = w;
     }
 }
-// What the 64 slots from k0 on had: lane (col < 4, h) those of keys 16 col + 4 h ..  Requested with the keys, a tile ahead: a load
-// behind the next tile's would be waited for together with it.
-struct Had {
-    float x[4];
-    __device__ __forceinline__ void request(const float* had, int k0, int width, int lane) {
-        const int key = k0 + 16 * (lane & 15) + 4 * (lane >> 4);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = had != nullptr && (lane & 15) < 4 && key + r < width ? had[key + r] : 0.0f;
-    }
-};
-// adds up the columns and writes the 64 sums
-__device__ __forceinline__ void put_weights(float (&sum)[4][4], unsigned bad, const Had& had, float* out, int k0, int width, int lane) {
+// the sums of a tile's 64 keys over the lanes of a column, in LDS; pieces without a page get none
+__device__ __forceinline__ void put_sums(const float (&sum)[4], unsigned bad, float* to, int lane) {
     const int col = lane & 15, h = lane >> 4;
-    float mine[4] = {};
+    float mine = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float x = over_columns(sum[j][r]);
-            mine[r] = col == j ? x : mine[r];
-        }
-    if (col >= 4) return;
-    const int key = k0 + 16 * col + 4 * h;
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-        if (key + r < width) out[key + r] = had.x[r] + (bad >> col & 1 ? 0.0f : mine[r]);
+    for (int j = 0; j < 4; ++j) {
+        const float x = over_h(sum[j], true);
+        mine = h == j ? x : mine;
+    }
+    to[16 * h + col] = bad >> h & 1 ? 0.0f : mine;
+}
+// a workgroup's sums for the slots [begin, end), of which no query sees those from `seen` on, added to what they had
+__device__ __forceinline__ void add_sums(const float* sums, const float* had, float* to, int begin, int end, int seen) {
+    __syncthreads();
+    for (int key = begin + threadIdx.x; key < end; key += WAVES * 64)
+        to[key] = (had != nullptr ? had[key] : 0.0f) + (key < seen ? sums[key - begin] : 0.0f);
 }
 }  // namespace
 
 // At most 16 rows (a decoding step): their operands stay in registers, a wavefront walks tiles of keys, the next one on its way.
 template <int D, int NG>
-__global__ void __launch_bounds__(WAVES * 64) cache4_weights_few_kernel(Cache4 c, CacheQueries q, const float* __restrict__ lse,
+__global__ void __launch_bounds__(WAVES * 64, 4) cache4_weights_few_kernel(Cache4 c, CacheQueries q, const float* __restrict__ lse,
                                                                         const float* __restrict__ weights, float* __restrict__ out, int width, int chunk) {
     __shared__ __attribute__((aligned(16))) _Float16 s_ks[WAVES][TILE * NG];
+    // (the sums wait here for one pass at the end: stores between the tiles would be waited for with the next tile's loads)
+    __shared__ __attribute__((aligned(16))) float s_sum[FEW_CHUNK];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
     const int slab = blockIdx.y, b = slab / c.heads, head = slab - b * c.heads, share = q.Hq / c.heads;
     const RowRange range(c, q, b, share);
     const int last_end = range.rows > 0 ? range.end(range.count - 1, q.causal) : 0;
-    const float* const had = weights != nullptr ? weights + (size_t)slab * width : nullptr;
-    float* const to = out + (size_t)slab * width;
     constexpr int NEXT = TILE * WAVES;
-    const int k_end = min((int)(blockIdx.x + 1) * chunk, width), seen = min(k_end, last_end);
-    int k0 = blockIdx.x * chunk + TILE * wave;
+    const int k_begin = blockIdx.x * chunk, k_end = min(k_begin + chunk, width), seen = min(k_end, last_end);
+    int k0 = k_begin + TILE * wave;
     typedef KeyTile<D, NG, false> Tile;
     Tile tile;
-    Had next_had;
     PageIds pages;
     const int* const table = c.table + (size_t)b * c.columns;
     const unsigned char* const head_at = c.data + head * c.block_bytes();
     if (k0 < seen) {
         pages.look_up(c, table, k0);
-        next_had.request(had, k0, width, lane);
         tile.request(c, head_at, pages, k0, lane);
         pages.look_up(c, table, k0 + NEXT);
         const int row = min(col, range.rows - 1), tq = row / share, g = row - tq * share;
-        const int end = col < range.rows ? range.end(tq, q.causal) : 0;
         const int first_end = range.end(0, q.causal);
         Queries4<D> query;
         const float sc = query.load(q, b * q.strides.b + (head * share + g) * q.strides.h + tq * q.strides.n, h);
-        // (columns without a row leave no weight either)
+        // (of 16 rows those that are not there leave no weight either)
         const float reference = col < range.rows ? row_reference(lse[((size_t)b * q.Hq + head * share + g) * q.Nq + tq]) : __builtin_inff();
+        const int end = col < range.rows ? range.end(tq, q.causal) : 0;
+        LaneRows rows;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            rows.sc[r] = __shfl(sc, 4 * h + r, 64);
+            rows.reference[r] = __shfl(reference, 4 * h + r, 64);
+            rows.end[r] = __shfl(end, 4 * h + r, 64);
+        }
         for (; k0 < seen; k0 += NEXT) {
             wave_order();
             *(typename Tile::scale_t*)(s_ks[wave] + lane * NG) = tile.ks;
             wave_order();
-            KeyOperands<D, NG> keys;
-            keys.make(tile, s_ks[wave], h);
+            typename Tile::words words[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) words[j] = tile.k[j];
             const unsigned bad = tile.bad;
-            const Had now_had = next_had;
             if (k0 + NEXT < seen) {
-                next_had.request(had, k0 + NEXT, width, lane);
                 tile.request(c, head_at, pages, k0 + NEXT, lane);
                 pages.look_up(c, table, k0 + 2 * NEXT);
             }
-            float sum[4][4] = {};
-            add_weights<D, NG>(sum, keys, query.op, sc, reference, end - k0, k0 + TILE <= first_end, h);
-            put_weights(sum, bad, now_had, to, k0, width, lane);
+            // (a piece at a time: with the operands of all 64 keys in registers two wavefronts fit on a SIMD instead of four)
+            float sum[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                half8 k[D / 32];
+                LaneScales<NG> ks;
+                lane_scales<NG>(s_ks[wave], 16 * j + col, ks);
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) k[i] = operand(words[j][i]);
+                sum[j] = piece_weights<D, NG>(query.op, k, ks, rows, k0 + 16 * j + col, k0 + TILE <= first_end);
+            }
+            put_sums(sum, bad, s_sum + (k0 - k_begin), lane);
         }
     }
-    // slots that no query sees keep what they had
-    for (; k0 < k_end; k0 += NEXT) {
-        const int key = k0 + lane;
-        if (key < width) to[key] = had != nullptr ? had[key] : 0.0f;
-    }
+    add_sums(s_sum, weights != nullptr ? weights + (size_t)slab * width : nullptr, out + (size_t)slab * width, k_begin, k_end, seen);
 }
 
 // More rows: a workgroup takes 256 keys, a wavefront 64 of them, whose operands stay in its registers.  The rows come 64 at a time:
@@ -1012,21 +993,19 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache4_weights_kernel(Cache4 c,
                                                                        const float* __restrict__ weights, float* __restrict__ out, int width) {
     __shared__ __attribute__((aligned(16))) _Float16 s_ks[WAVES][TILE * NG];
     __shared__ half8 s_q[WAVES][D / 32][64];
-    __shared__ float s_sc[WAVES][16], s_reference[WAVES][16];
-    __shared__ int s_end[WAVES][16];
+    __shared__ __attribute__((aligned(16))) float s_sum[WAVES * TILE];
+    __shared__ __attribute__((aligned(16))) float s_sc[WAVES][16], s_reference[WAVES][16];
+    __shared__ __attribute__((aligned(16))) int s_end[WAVES][16];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
     const int slab = blockIdx.y, b = slab / c.heads, head = slab - b * c.heads, share = q.Hq / c.heads;
     const RowRange range(c, q, b, share);
     const int last_end = range.rows > 0 ? range.end(range.count - 1, q.causal) : 0;
-    const float* const had = weights != nullptr ? weights + (size_t)slab * width : nullptr;
-    float* const to = out + (size_t)slab * width;
     const int k_first = blockIdx.x * WAVES * TILE, k0 = k_first + wave * TILE;
-    float sum[4][4] = {};
+    float sum[4] = {};
     unsigned bad = 0;
-    Had its_had;
-    its_had.request(had, k0, width, lane);
     if (k_first < last_end) {                   // (the same for the whole workgroup)
-        KeyOperands<D, NG> keys;
+        half8 k[4][D / 32];
+        LaneScales<NG> ks[4];
         {
             PageIds pages;
             pages.look_up(c, c.table + (size_t)b * c.columns, k0);
@@ -1035,7 +1014,12 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache4_weights_kernel(Cache4 c,
             *(typename ScaleWord<NG>::type*)(s_ks[wave] + lane * NG) = tile.ks;
             bad = tile.bad;
             wave_order();
-            keys.make(tile, s_ks[wave], h);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                lane_scales<NG>(s_ks[wave], 16 * j + col, ks[j]);
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) k[j][i] = operand(tile.k[j][i]);
+            }
         }
         // the first row that sees a key of the workgroup
         int row0 = 0;
@@ -1062,11 +1046,22 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache4_weights_kernel(Cache4 c,
                 half8 op[D / 32];
 #pragma unroll
                 for (int i = 0; i < D / 32; ++i) op[i] = s_q[w][i][lane];
-                add_weights<D, NG>(sum, keys, op, s_sc[w][col], s_reference[w][col], s_end[w][col] - k0, k0 + TILE <= first_end, h);
+                LaneRows rows;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    rows.sc[r] = s_sc[w][4 * h + r];
+                    rows.reference[r] = s_reference[w][4 * h + r];
+                    rows.end[r] = s_end[w][4 * h + r];
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    sum[j] += piece_weights<D, NG>(op, k[j], ks[j], rows, k0 + 16 * j + col, k0 + TILE <= first_end);
             }
         }
     }
-    if (k0 < width) put_weights(sum, bad, its_had, to, k0, width, lane);
+    put_sums(sum, bad, s_sum + wave * TILE, lane);
+    add_sums(s_sum, weights != nullptr ? weights + (size_t)slab * width : nullptr, out + (size_t)slab * width, k_first, min(k_first + WAVES * TILE, width),
+             last_end);
 }
 
 namespace {
@@ -1149,7 +1144,7 @@ hipError_t launch_cache4_weights(const Cache4& c, const CacheQueries& q, const f
     int chunks = few ? WANTED_FEW / slabs : tiles;
     if (chunks < 1) chunks = 1;
     if (chunks > tiles) chunks = tiles;
-    const int chunk = (tiles + chunks - 1) / chunks * WAVES * TILE;
+    const int longest = few ? FEW_CHUNK : WAVES * TILE, even = (tiles + chunks - 1) / chunks * WAVES * TILE, chunk = even < longest ? even : longest;
     const dim3 grid((width + chunk - 1) / chunk, slabs);
 #define SAGE_CACHE4_WEIGHTS(D, NG)                                                                                          \
     do {                                                                                                                     \
