@@ -44,8 +44,15 @@ __device__ __forceinline__ void put_row8(void* p, long at, const float (&x)[8]) 
         *(b8*)((__bf16*)p + at) = v;
     }
 }
-// the scale of a group from its largest magnitude
-__device__ __forceinline__ _Float16 scale_of(float amax) { return (_Float16)__builtin_fminf(amax / 7.0f, MAX_SCALE); }
+// The quotient z / d, rounded as a division rounds it, by three instructions instead of ten: with y within 2^-22 of 1 / d, q = z y
+// is off by three ulp at most, its remainder z - q d is exact in an FMA where d has few bits (a scale in fp16, 7), and q +
+// remainder y rounds to the quotient -- which lies 2^-12 ulp and more from where two fp32 numbers meet, or on one of them.
+__device__ __forceinline__ float quotient(float z, float d, float y) {
+    const float q = z * y;
+    return __builtin_fmaf(__builtin_fmaf(-q, d, z), y, q);
+}
+// the scale of a group from its largest magnitude (infinite: the quotient is no number, and the minimum passes over it)
+__device__ __forceinline__ _Float16 scale_of(float amax) { return (_Float16)__builtin_fminf(quotient(amax, 7.0f, 1.0f / 7.0f), MAX_SCALE); }
 // where channel e of 8 stands in its word
 template <bool IS_K> __device__ __forceinline__ int nibble_shift(int e) { return IS_K ? 4 * (e >> 1) + 16 * (e & 1) : 4 * e; }
 // the word of octet o (channels 8 o .. 8 o + 7) in its row
@@ -58,23 +65,17 @@ __device__ __forceinline__ float group_max(const float (&x)[8]) {
     for (int e = 0; e < 8; ++e) m = __builtin_fmaxf(m, __builtin_fabsf(x[e]));
     return lanes_max<GROUP / 8>(m);
 }
-// The codes of 8 channels in their word.  The quotient x / delta to the last bit by three instructions per channel instead of a
-// division's ten (which were most of the call): with y = 1 / delta correctly rounded, q = x y is off by an ulp at most, its
-// remainder x - q delta is exact in an FMA, and q + remainder y rounds to the quotient.  Limited to 8 steps before that, so that
-// infinities saturate and nothing overflows; the addition of 1.5 * 2^23 + 8 rounds to whole numbers, ties to even, and leaves
-// code + 8 in the low bits.
+// The codes of 8 channels in their word: limited to 7 steps before the quotient, so that infinities saturate and nothing
+// overflows; the addition of 1.5 * 2^23 + 8 rounds to whole numbers, ties to even, and leaves code + 8 in the low bits.
 template <bool IS_K>
 __device__ __forceinline__ unsigned pack8(const float (&x)[8], float delta) {
-    const float y = delta > 0.0f ? 1.0f / delta : 0.0f, most = 8.0f * delta;
+    const float y = delta > 0.0f ? __builtin_amdgcn_rcpf(delta) : 0.0f, most = 7.0f * delta;
     unsigned n[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float z = __builtin_amdgcn_fmed3f(x[e], -most, most), q = z * y;
-        const float exact = __builtin_fmaf(__builtin_fmaf(-q, delta, z), y, q);
-        n[e] = __builtin_bit_cast(unsigned, __builtin_amdgcn_fmed3f(exact, -7.0f, 7.0f) + 12582920.0f);
-    }
-    // two nibbles in the low byte of a word, four of those to a word
-    auto pair = [&n](int i, int j) { return (n[i] & 15u) | n[j] << 4; };
+    for (int e = 0; e < 8; ++e)
+        n[e] = __builtin_bit_cast(unsigned, quotient(__builtin_amdgcn_fmed3f(x[e], -most, most), delta, y) + 12582920.0f);
+    // two nibbles in the low byte of a word (1 .. 15 is all of it), four of those to a word
+    auto pair = [&n](int i, int j) { return n[j] << 4 | n[i]; };
     const unsigned b0 = IS_K ? pair(0, 2) : pair(0, 1), b1 = IS_K ? pair(4, 6) : pair(2, 3);
     const unsigned b2 = IS_K ? pair(1, 3) : pair(4, 5), b3 = IS_K ? pair(5, 7) : pair(6, 7);
     return __builtin_amdgcn_perm(b1, b0, 0x0c0c0400u) | __builtin_amdgcn_perm(b3, b2, 0x04000c0cu);
@@ -96,21 +97,23 @@ __device__ __forceinline__ void unpack8(unsigned w, float delta, float (&x)[8]) 
 }
 }  // namespace
 
-// A thread takes 8 channels of K and of V of a token, D / 8 adjacent threads the token's row.
+// A thread takes 8 channels of K and of V of a token, D / 8 adjacent threads the token's row.  24.6K tokens of 8 heads of 128 in bf16,
+// 166 MB read and written: 43 us; the same loads and stores without the arithmetic 34.  (Two tokens per thread, or the heads of a
+// token next to each other in the grid: no change.)
 template <int D, int GROUP, int TYPE>
 __global__ void __launch_bounds__(256) cache4_append_kernel(Cache4 c, const void* __restrict__ k, RowStrides ks, const void* __restrict__ v,
                                                             RowStrides vs, const float* __restrict__ k_mean, const int* __restrict__ start,
                                                             const int* __restrict__ count, int N) {
     constexpr int OCTETS = D / 8, ROWS = 256 / OCTETS;
     const int o = threadIdx.x % OCTETS, bh = blockIdx.y, b = bh / c.heads, h = bh - b * c.heads;
-    const int n = blockIdx.x * ROWS + threadIdx.x / OCTETS;
+    const int first = blockIdx.x * ROWS, row = threadIdx.x / OCTETS, n = first + row;
     const int there = count != nullptr ? min(count[b], N) : N;
     // (a row's threads stay or leave together: group_max looks at no other row's)
     if (n >= there) return;
     // the rows are on their way while the page is looked up
     float x[8], y[8];
-    row8<TYPE>(k, b * ks.b + h * ks.h + n * ks.n + 8 * o, x);
-    row8<TYPE>(v, b * vs.b + h * vs.h + n * vs.n + 8 * o, y);
+    row8<TYPE>(k, (b * ks.b + h * ks.h + first * ks.n) + row * ks.n + 8 * o, x);
+    row8<TYPE>(v, (b * vs.b + h * vs.h + first * vs.n) + row * vs.n + 8 * o, y);
     float mean[8] = {};
     if (k_mean != nullptr) {
 #pragma unroll
@@ -163,10 +166,10 @@ __global__ void __launch_bounds__(256) cache4_load_kernel(Cache4 c, const int* _
 
 #define SAGE_CACHE4_SHAPE(KERNEL, TYPE, ...)                                                                       \
     do {                                                                                                            \
-        if (c.D == 64 && c.group == 32) KERNEL<64, 32, TYPE><<<grid, 256, 0, st>>>(__VA_ARGS__);                    \
+        if (c.D == 64 && c.groups == 2) KERNEL<64, 32, TYPE><<<grid, 256, 0, st>>>(__VA_ARGS__);                    \
         else if (c.D == 64) KERNEL<64, 64, TYPE><<<grid, 256, 0, st>>>(__VA_ARGS__);                                \
-        else if (c.group == 32) KERNEL<128, 32, TYPE><<<grid, 256, 0, st>>>(__VA_ARGS__);                           \
-        else if (c.group == 64) KERNEL<128, 64, TYPE><<<grid, 256, 0, st>>>(__VA_ARGS__);                           \
+        else if (c.groups == 4) KERNEL<128, 32, TYPE><<<grid, 256, 0, st>>>(__VA_ARGS__);                           \
+        else if (c.groups == 2) KERNEL<128, 64, TYPE><<<grid, 256, 0, st>>>(__VA_ARGS__);                           \
         else KERNEL<128, 128, TYPE><<<grid, 256, 0, st>>>(__VA_ARGS__);                                             \
     } while (0)
 
@@ -336,7 +339,7 @@ __global__ void __launch_bounds__(256) cache4_gather_kernel(Cache4 c, Cache4 to,
     constexpr int TPR = D / 16, ROWS = 256 / TPR;
     typedef unsigned u4 __attribute__((ext_vector_type(4)));
     const int bh = blockIdx.y, b = bh / c.heads, h = bh - b * c.heads, i = threadIdx.x % TPR;
-    const int j0 = blockIdx.x * ROWS * GATHER_ROWS + threadIdx.x / TPR, S = c.scales(), half = D / 32;
+    const int j0 = blockIdx.x * ROWS * GATHER_ROWS + threadIdx.x / TPR, S = c.groups, half = D / 32;
     const bool is_v = i >= half;
     const int chunk = is_v ? i - half : i;
     int from[GATHER_ROWS];

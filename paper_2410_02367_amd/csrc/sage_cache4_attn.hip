@@ -108,7 +108,8 @@ struct Queries4 {
         for (int i = 0; i < D / 32; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) op[i][e] = (_Float16)ldexpf(x[i][e], 14 - exponent - (e & 2 ? 4 : 0));
-        return __builtin_fmaxf(ldexpf(q.sm_scale * LOG2E, exponent - 14), 1e-37f);
+        // (never 0 or infinite: a score of 0 or -infinity times it stays one)
+        return __builtin_fminf(__builtin_fmaxf(ldexpf(q.sm_scale * LOG2E, exponent - 14), 1e-37f), 1e37f);
     }
 };
 
@@ -148,7 +149,7 @@ struct KeyTile {
     // head: the block of the key head in page 0
     static __device__ __forceinline__ const unsigned char* block(const Cache4& c, const unsigned char* head, int id, bool& ok) {
         ok = (unsigned)id < (unsigned)c.num_pages;
-        return head + (size_t)(unsigned)__builtin_amdgcn_readfirstlane(ok ? id : 0) * (c.heads * c.block_bytes());
+        return head + (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane(ok ? id : 0) * c.page_bytes;
     }
     __device__ __forceinline__ void request(const Cache4& c, const unsigned char* head, const PageIds& pages, int k0, int lane) {
         const int col = lane & 15, h = lane >> 4, mask = c.page() - 1;
@@ -398,7 +399,7 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
 
     Lds& mine = *(Lds*)(lds + wave * sizeof(Lds));
     const int* const table = c.table + (size_t)b * c.columns;
-    const unsigned char* const head_at = c.data + head * c.block_bytes();
+    const unsigned char* const head_at = c.data + (size_t)head * c.block_bytes;
     typedef KeyTile<D, NG, true> Tile;
     typedef typename Tile::words words;
     constexpr int NEXT = TILE * WAVES;
@@ -621,7 +622,7 @@ cache4_attn_rows_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStr
     }
 
     const int* const table = c.table + (size_t)b * c.columns;
-    const unsigned char* const head_at = c.data + head * c.block_bytes();
+    const unsigned char* const head_at = c.data + (size_t)head * c.block_bytes;
     TileShare<D, NG> own;
     PageIds pages;
     // the share that has arrived, the tile from k0 on, into a buffer
@@ -938,7 +939,7 @@ __global__ void __launch_bounds__(WAVES * 64, 4) cache4_weights_few_kernel(Cache
     Tile tile;
     PageIds pages;
     const int* const table = c.table + (size_t)b * c.columns;
-    const unsigned char* const head_at = c.data + head * c.block_bytes();
+    const unsigned char* const head_at = c.data + (size_t)head * c.block_bytes;
     if (k0 < seen) {
         pages.look_up(c, table, k0);
         tile.request(c, head_at, pages, k0, lane);
@@ -1010,7 +1011,7 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache4_weights_kernel(Cache4 c,
             PageIds pages;
             pages.look_up(c, c.table + (size_t)b * c.columns, k0);
             KeyTile<D, NG, false> tile;
-            tile.request(c, c.data + head * c.block_bytes(), pages, k0, lane);
+            tile.request(c, c.data + (size_t)head * c.block_bytes, pages, k0, lane);
             *(typename ScaleWord<NG>::type*)(s_ks[wave] + lane * NG) = tile.ks;
             bad = tile.bad;
             wave_order();
@@ -1118,7 +1119,7 @@ hipError_t launch_cache4_attn(const Cache4& c, const CacheQueries& q, void* out,
     const size_t rows = (size_t)q.B * q.Hq * q.Nq;
     float* const part = p.n_splits > 1 ? (float*)workspace : nullptr;
     float* const part_lse = p.n_splits > 1 ? part + p.n_splits * rows * c.D : nullptr;
-    const int ng = c.scales();
+    const int ng = c.groups;
     if (c.D == 64) {
         if (ng == 1) launch_attn_form<64, 1>(p, c, q, out, os, lse, part, part_lse, st);
         else launch_attn_form<64, 2>(p, c, q, out, os, lse, part, part_lse, st);
@@ -1138,7 +1139,7 @@ hipError_t launch_cache4_attn(const Cache4& c, const CacheQueries& q, void* out,
 
 hipError_t launch_cache4_weights(const Cache4& c, const CacheQueries& q, const float* lse, const float* weights, float* out, int width,
                                  hipStream_t st) {
-    const int slabs = q.B * c.heads, ng = c.scales(), tiles = (width + WAVES * TILE - 1) / (WAVES * TILE);
+    const int slabs = q.B * c.heads, ng = c.groups, tiles = (width + WAVES * TILE - 1) / (WAVES * TILE);
     const bool few = q.Hq / c.heads * q.Nq <= 16;
     // few rows: as many workgroups as the attention has, so that a wavefront has tiles to walk
     int chunks = few ? WANTED_FEW / slabs : tiles;

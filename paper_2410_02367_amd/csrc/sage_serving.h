@@ -23,22 +23,21 @@ struct Cache4 {
     const int* table;           // [B, columns]; an entry outside 0 .. num_pages - 1 holds no tokens
     int num_pages, columns, heads;
     int shift;                  // log2 of the tokens per page
-    int D, group;
+    int D, groups;              // channels, and groups of them with a scale
+    unsigned block_bytes, page_bytes;           // of a head of a page, of a page: (D + 4 groups) << shift, times the heads
     __host__ __device__ int page() const { return 1 << shift; }
-    __host__ __device__ int scales() const { return D / group; }
     __host__ __device__ int capacity() const { return columns << shift; }
-    __host__ __device__ size_t block_bytes() const { return (size_t)(D + 4 * scales()) << shift; }
     // the block that holds token `slot` of sequence b, or null
     __device__ unsigned char* block(int b, int h, int slot) const {
         const int p = table[(size_t)b * columns + (slot >> shift)];
         if ((unsigned)p >= (unsigned)num_pages) return nullptr;
-        return data + ((size_t)p * heads + h) * block_bytes();
+        return data + (size_t)h * block_bytes + (unsigned long long)(unsigned)p * page_bytes;
     }
     // byte offsets in a block of the parts of row r (of its page)
     __device__ int k_codes(int r) const { return r * (D / 2); }
     __device__ int v_codes(int r) const { return ((D / 2) << shift) + r * (D / 2); }
-    __device__ int k_scales(int r) const { return (D << shift) + r * 2 * scales(); }
-    __device__ int v_scales(int r) const { return ((D + 2 * scales()) << shift) + r * 2 * scales(); }
+    __device__ int k_scales(int r) const { return (D << shift) + r * 2 * groups; }
+    __device__ int v_scales(int r) const { return ((D + 2 * groups) << shift) + r * 2 * groups; }
 };
 
 // [b][h][n] rows of a tensor rotated; x and y may be the same.  All return the hipError_t of the launch.

@@ -44,7 +44,9 @@ int check_cache(const void* cache, const int32_t* pages, int B, int Hkv, int D, 
     return SAGE_OK;
 }
 sage::Cache4 view(const void* cache, const int32_t* pages, int Hkv, int D, int num_pages, int columns, int page, int group) {
-    return {(unsigned char*)cache, pages, num_pages, columns, Hkv, __builtin_ctz((unsigned)page), D, group};
+    // (at most 65535 heads of 256 rows of 144 bytes: below 2^32)
+    const unsigned block = (unsigned)sage_cache4_block_bytes(D, page, group);
+    return {(unsigned char*)cache, pages, num_pages, columns, Hkv, __builtin_ctz((unsigned)page), D, D / group, block, block * (unsigned)Hkv};
 }
 int check_queries(int B, int Hq, int Hkv, int Nq, int type, float sm_scale) {
     if (int e = check_shape(B, Hq, Nq)) return e;
