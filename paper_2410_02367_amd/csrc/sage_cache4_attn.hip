@@ -307,12 +307,19 @@ __device__ __forceinline__ float over_h(float x, bool sum) {
 }  // namespace
 
 namespace {
-// Which (sequence, head), tile of rows and chunk of keys a workgroup has: slabs dealt out to the XCDs, so that the workgroups of one
-// share its keys in one L2; the tiles that see most first.
+// Which (sequence, head), tile of rows and chunk of keys a workgroup has.  One tile of rows: nothing is shared, the first chunks of
+// all slabs come first and the last ones, which short sequences do not have, fill up behind them.  Several: slabs dealt out to the
+// XCDs, so that the workgroups of one share its keys in one L2; the tiles that see most first.
 struct RowsPlace {
     int slab, tile, split, slabs;
     __device__ __forceinline__ RowsPlace(const Cache4& c, const CacheQueries& q, int tiles, int n_splits) {
         slabs = q.B * c.heads;
+        if (tiles == 1) {
+            slab = blockIdx.x % slabs;
+            split = blockIdx.x / slabs;
+            tile = 0;
+            return;
+        }
         const int per_slab = tiles * n_splits;
         int rest;
         if (slabs % 8 == 0) {
@@ -1068,7 +1075,8 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache4_weights_kernel(Cache4 c,
 namespace {
 // How a call is cut.  Keys: chunks of a multiple of 256, as many as it takes to have WANTED workgroups, two per compute unit (us with
 // 256 / 512 / 1024 workgroups: 256 slabs of 16K keys 146 / 112 / 110, 8 of 128K 40 / 36 / 40, 64 of 16K with 64 rows 110 / 90 / 98), none
-// shorter than 512 unless the caller asks for it.  Rows: 16 or 32 per workgroup, whose wavefronts share the keys; or 128, whose
+// shorter than 512 unless the caller asks for it.  Sequences of a batch differ in length: up to four times as many chunks of 2048 keys
+// even that out (256 slabs of 8K to 16K keys: 2 chunks 117, 8 chunks 106; all of 16K: 126 and 122).  Rows: 16 or 32 per workgroup, whose wavefronts share the keys; or 128, whose
 // wavefronts share the operands, where there are that many and the chunks are long (us with 32 / 128: 4096 rows of 8 slabs of 32K
 // keys 1117 / 934, of 4K 117 / 111, 128 rows of 64 slabs of 16K 125 / 108; chunks of 512 keys: 512 rows of 32 slabs of 2K 42 / 49).
 struct AttnPlan {
@@ -1081,9 +1089,14 @@ AttnPlan plan(int B, int Hq, int Hkv, int Nq, int capacity, int requested) {
         AttnPlan p;
         p.rows = per;
         p.tiles = (rows + per - 1) / per;
-        long n = requested > 0 ? requested : WANTED / ((long)B * Hkv * p.tiles);
+        const long groups = (long)B * Hkv * p.tiles;
+        long n = requested > 0 ? requested : WANTED / groups;
         const int least = requested > 0 ? 256 : 512;
         if (n > capacity / least) n = capacity / least;
+        if (requested == 0 && B > 1 && p.tiles == 1) {
+            const long more = 4 * WANTED / groups, most = capacity / LONG_CHUNK;
+            n = n > more || n > most ? n : more < most ? more : most;
+        }
         if (n < 1) n = 1;
         p.chunk = (int)(((capacity + n - 1) / n + 255) / 256 * 256);
         p.n_splits = (capacity + p.chunk - 1) / p.chunk;
