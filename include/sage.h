@@ -468,8 +468,9 @@ int sage_cache4_load(const void* cache, const int32_t* pages, const int32_t* sta
 
 /*
  * Attention of new queries over the cache, softmax(sm_scale q K^T) V with K and V as the cache holds them: FP16 products of the
- * codes with fp32 accumulation (q is not quantized), the scales applied to the sums.  Query head hq reads key head
- * hq / (Hq / Hkv).
+ * codes with fp32 accumulation (q is not quantized), the scales applied to the sums; a weight times a scale of V is rounded to
+ * fp16 for the second product.  Query head hq reads key head hq / (Hq / Hkv).  Scores up to 2^27 (in the exponent of 2).  A query
+ * that is no number leaves the others alone.
  *   q        in   [B,Hq,Nq,D] SAGE_F16 or SAGE_BF16;  out  out, the same type and shape, fully overwritten
  *   lengths  in   [B] int32: tokens of the sequence in the cache (the queries' own among them); limited to 0 .. columns * page
  *   count    in   [B] int32, or NULL: Nq.  Sequence b has the queries t < count[b]; the rows behind them become zeros
@@ -477,7 +478,7 @@ int sage_cache4_load(const void* cache, const int32_t* pages, const int32_t* sta
  *            no key has the output 0
  *   lse      out  [B,Hq,Nq] fp32, or NULL: ln of the sum of exp(sm_scale q K^T), -infinity without a key.  (K as the cache holds
  *            it: a k_mean moves it by sm_scale q . k_mean)
- *   n_splits   how many workgroups share a row's keys, 0: chosen from the shape
+ *   n_splits   how many workgroups share a row's keys (at most the table's tokens / 256), 0: chosen from the shape
  *   workspace  device, >= sage_cache4_attn_workspace() bytes (same arguments), 16-byte aligned; scratch, contents undefined
  *              on entry and exit; may be NULL when that size is 0.  Two calls that share one are ordered by the caller
  */
@@ -492,7 +493,8 @@ int sage_cache4_attn(const void* q, const int64_t* q_strides, const void* cache,
  *     out[b][h][s] = weights[b][h][s] + sum over the query heads of key head h and the queries that see slot s of
  *                                       exp(sm_scale q K^T - lse),
  * the sum in fp32, in an order that does not change from call to call.
- *   lse      in   from sage_cache4_attn with the same arguments (a row whose lse is -infinity adds nothing)
+ *   lse      in   from sage_cache4_attn with the same arguments (a row whose lse is -infinity adds nothing).  The weights
+ *            of a row sum to 1
  *   weights  in   [B,Hkv,width] fp32, or NULL: zeros;  out  out, the same shape, may be weights itself; width >= columns * page.
  *            Slots from lengths[b] on keep their value
  */
@@ -507,7 +509,8 @@ int sage_cache4_weights(const void* q, const int64_t* q_strides, const void* cac
  * of them where there are no more than keep.  Their rows are copied, in order, to slots 0, 1, ... of the pages in out_pages; the
  * old pages are only read.  Heads of a sequence keep tokens of their own.
  *   out_cache, out_num_pages   the pool of the new pages: the same pool or another one of the same form;  out_pages
- *            [B, out_columns], none of them a page that `pages` names, out_columns * page >= keep
+ *            [B, out_columns], none of them (of the same pool) a page that `pages` names -- the kernels cannot see that
+ *            --, out_columns * page >= keep
  *   weights  in   [B,Hkv,width];  out_weights  out  [B,Hkv,out_width], out_width >= keep: the kept tokens' weights, then zeros
  *   kept     out  [B,Hkv,keep] int32: the slots that were kept, ascending, then -1
  *   out_lengths  out  [B] int32: min(lengths[b], keep)

@@ -1110,6 +1110,11 @@ AttnPlan plan(int B, int Hq, int Hkv, int Nq, int capacity, int requested) {
 }
 }  // namespace
 
+long long cache4_attn_workgroups(int B, int Hq, int Hkv, int Nq, int capacity, int n_splits) {
+    const AttnPlan p = plan(B, Hq, Hkv, Nq, capacity, n_splits);
+    return (long long)B * Hkv * p.tiles * p.n_splits;
+}
+
 size_t cache4_attn_workspace(int B, int Hq, int Hkv, int Nq, int D, int capacity, int n_splits) {
     const AttnPlan p = plan(B, Hq, Hkv, Nq, capacity, n_splits);
     return p.n_splits <= 1 ? 0 : (size_t)p.n_splits * B * Hq * Nq * (D + 1) * sizeof(float);

@@ -131,6 +131,7 @@ int sage_cache4_load(const void* cache, const int32_t* pages, const int32_t* sta
 size_t sage_cache4_attn_workspace(int B, int Hq, int Hkv, int Nq, int D, int columns, int page, int n_splits) {
     if (check_shape(B, Hq, Nq) || check_shape(B, Hkv, 1) || Hq % Hkv != 0 || (D != 64 && D != 128) || !page_ok(page)) return 0;
     if (columns <= 0 || (long long)columns * page > (1 << 23) || n_splits < 0) return 0;
+    if ((long long)Hq * Nq > (1 << 30) || (long long)B * Hq * Nq > 0x7fffffffLL) return 0;
     return sage::cache4_attn_workspace(B, Hq, Hkv, Nq, D, columns * page, n_splits);
 }
 
@@ -141,6 +142,8 @@ int sage_cache4_attn(const void* q, const int64_t* q_strides, const void* cache,
     if (int e = check_cache(cache, pages, B, Hkv, D, num_pages, columns, page, group)) return e;
     if (int e = check_queries(B, Hq, Hkv, Nq, type, sm_scale)) return e;
     if (n_splits < 0) return SAGE_ERR_VALUE;
+    // (workgroups are counted in an int by the kernels)
+    if (sage::cache4_attn_workgroups(B, Hq, Hkv, Nq, columns * page, n_splits) > (1ll << 30)) return SAGE_ERR_SHAPE;
     const size_t need = sage_cache4_attn_workspace(B, Hq, Hkv, Nq, D, columns, page, n_splits);
     if (need > 0 && !workspace) return SAGE_ERR_NULL;
     if (workspace_bytes < need) return SAGE_ERR_WORKSPACE;

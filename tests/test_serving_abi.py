@@ -95,6 +95,69 @@ def test_attention_and_weights_refusals(lib):
         assert lib.sage_cache4_attn_workspace(*bad) == 0
 
 
+def test_workgroups_beyond_what_the_kernels_count(lib):
+    args = dict(B=64, Hq=1 << 10, Hkv=1, Nq=1 << 15)
+    def attn(splits, columns):
+        return lib.sage_cache4_attn(GOOD, None, GOOD, GOOD, GOOD, None, GOOD, None, None, GOOD, 1 << 62, args["B"], args["Hq"], args["Hkv"], args["Nq"], 64,
+                                    0, 1 << 20, columns, 256, 32, 1, F(0.125), splits, None)
+    assert args["B"] * args["Hq"] * args["Nq"] == 1 << 31 and attn(1, 1) == 2                # rows
+    args["B"] = 32
+    assert attn(1 << 15, 1 << 15) == 2                                                       # 2^26 and more tiles of rows times 2^15 chunks
+    assert lib.sage_cache4_attn_workspace(64, 1 << 10, 1, 1 << 15, 64, 1, 256, 0) == 0
+
+
+def test_workspace_holds_the_partial_results(lib):
+    # [chunks][rows] of D fp32 numbers and a logarithm; none for one chunk
+    assert lib.sage_cache4_attn_workspace(2, 8, 2, 1, 128, 64, 64, 1) == 0 and lib.sage_cache4_attn_workspace(2, 8, 2, 1, 128, 4, 64, 9) == 0
+    assert lib.sage_cache4_attn_workspace(2, 8, 2, 1, 128, 64, 64, 4) == 4 * 2 * 8 * 129 * 4
+    assert lib.sage_cache4_attn_workspace(1, 8, 2, 3, 64, 256, 16, 3) == 3 * 8 * 3 * 65 * 4
+    for splits in range(0, 40):
+        for columns, page in ((64, 64), (100, 16), (7, 256)):
+            n = lib.sage_cache4_attn_workspace(1, 4, 4, 1, 64, columns, page, splits) / (4 * 65 * 4)
+            assert n == int(n) and (n == 0 or 2 <= n <= max(2, columns * page // 256))
+
+
+SYMBOLIC = """
+import torch
+from torch._subclasses.fake_tensor import FakeTensorMode
+from torch.fx.experimental.symbolic_shapes import ShapeEnv
+from paper_2410_02367_amd import binding
+binding.load()
+native, env = binding._native, ShapeEnv()
+with FakeTensorMode(shape_env=env):
+    x = torch.empty(1, 2, env.create_unbacked_symint(), 64, dtype=torch.float16, device="cuda")
+    i, f, u = torch.empty(1, dtype=torch.int32, device="cuda"), torch.empty(4, dtype=torch.float64, device="cuda"), torch.empty(4, 2, 1152, dtype=torch.uint8, device="cuda")
+    p = torch.empty(1, env.create_unbacked_symint(), dtype=torch.int32, device="cuda")
+    assert native.rope(x, None, i, f, 0, 1.0, None, None, 0) is None and native.rope_bwd(x, x, i, f, 0, 1.0, None, None, 0) is None
+    assert native.cache4_append(x, x, u, p, i, None, None, 16, 32, 0) is None
+    assert native.cache4_load(u, p, None, 4, 64, None, None, 0, 16, 32, None, None, 0) is None
+    assert native.cache4_attn(x, u, p, i, None, 1, None, 16, 32, 0, 0, None, None, None, 0) is None
+    assert native.cache4_weights(x, u, p, i, x, None, None, 1, None, 16, 32, None, 0) is None
+    assert native.cache4_evict(u, p, i, x, u, p, 4, 0, 64, 16, 32, None, None, None, 0) is None
+print("all left to Python")
+"""
+
+
+def test_tensors_without_sizes_in_numbers_are_left_to_python(lib):
+    """In a process of its own, which is what an exception that passes through the interpreter would end."""
+    import os
+    import subprocess
+    import sys
+    run = subprocess.run([sys.executable, "-c", SYMBOLIC], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True,
+                         timeout=300)
+    assert run.returncode == 0 and "all left to Python" in run.stdout, (run.returncode, run.stderr[-500:])
+
+
+def test_the_extension_module_takes_no_arguments_that_are_not_in_order(lib):
+    import torch
+    from paper_2410_02367_amd import binding
+    n = binding._native
+    x = torch.zeros(1, 2, 4, 64, dtype=torch.float16)
+    for bad in ([], [x], [None] * 9, [x] * 9, [1] * 13, ["q"] * 15, [None] * 10, [x] * 13, [x] * 15, [object()] * 15, [x] * 10):
+        for f in (n.rope, n.rope_bwd, n.cache4_append, n.cache4_load, n.cache4_attn, n.cache4_weights, n.cache4_evict):
+            assert f(*bad) is None
+
+
 def test_evict_refusals(lib):
     other, third = ctypes.c_void_p(0x2000), ctypes.c_void_p(0x3000)
 
