@@ -418,7 +418,8 @@ enum { SAGE_F16 = 0, SAGE_BF16 = 1, SAGE_F32 = 2 };
  *   positions       in   int32; token n of sequence b is at positions[b * position_stride + n] (0: shared by all)
  *   inv_freq        in   [rotated / 2] fp64, radians per position: where a context is scaled, the scaled ones
  *   amplitude       multiplies the rotated channels (1; some scalings of the context use another); finite
- *   D a multiple of 8 up to 512, rotated even, 2 .. D; type SAGE_F16, SAGE_BF16 or SAGE_F32; B * (Hq + Hk) at most 65535
+ *   D a multiple of 8 up to 512, rotated even, 2 .. D; type SAGE_F16, SAGE_BF16 or SAGE_F32; B * (Hq + Hk) at most 65535,
+ *   B * N * D at most 512 * (2^24 - 1)
  * sage_rope_bwd takes the gradient of the outputs to the gradient of the inputs: the turn back, times amplitude.
  */
 int sage_rope(const void* q, const int64_t* q_strides, void* q_out, const int64_t* q_out_strides,
@@ -434,8 +435,8 @@ int sage_rope_bwd(const void* dq, const int64_t* dq_strides, void* dq_out, const
  * The cache: a pool [num_pages, Hkv, block] of bytes, block = sage_cache4_block_bytes(), each page `page` tokens of all heads,
  * and per sequence a row of the table `pages` [B, columns] int32: token slot s of sequence b lies in page
  * pages[b][s / page], row s % page.  An entry outside 0 .. num_pages - 1 holds no tokens: what is stored there is dropped, what
- * is read there is absent (no key for the attention, zeros for sage_cache4_load).  Pages that a call writes belong to one
- * sequence each.  Per token, head and group of channels Section 3.2's quantizer with 7 in place of 127,
+ * is read there is absent (no key for the attention, zeros for sage_cache4_load).  Pages that a call writes stand
+ * in its table once.  Per token, head and group of channels Section 3.2's quantizer with 7 in place of 127,
  *     delta = fp16(min(amax / 7, 65504)),  code = clamp(round_half_even(x / delta), -7, 7)   (fp32 divisions; delta = 0: 0),
  * where x is V, or fp32(K) - k_mean (Section 4.2: the attention does not change with a vector added to all keys of a head,
  * and K's channels carry a large one, which 4 bits have no room for).  A NaN is stored as 0, infinities as the largest value.
@@ -481,6 +482,7 @@ int sage_cache4_load(const void* cache, const int32_t* pages, const int32_t* sta
  *   n_splits   how many workgroups share a row's keys (at most the table's tokens / 256), 0: chosen from the shape
  *   workspace  device, >= sage_cache4_attn_workspace() bytes (same arguments), 16-byte aligned; scratch, contents undefined
  *              on entry and exit; may be NULL when that size is 0.  Two calls that share one are ordered by the caller
+ *   A call of 2^24 workgroups and more is refused (SAGE_ERR_SHAPE)
  */
 size_t sage_cache4_attn_workspace(int B, int Hq, int Hkv, int Nq, int D, int columns, int page, int n_splits);
 int sage_cache4_attn(const void* q, const int64_t* q_strides, const void* cache, const int32_t* pages, const int32_t* lengths,
@@ -493,8 +495,8 @@ int sage_cache4_attn(const void* q, const int64_t* q_strides, const void* cache,
  *     out[b][h][s] = weights[b][h][s] + sum over the query heads of key head h and the queries that see slot s of
  *                                       exp(sm_scale q K^T - lse),
  * the sum in fp32, in an order that does not change from call to call.
- *   lse      in   from sage_cache4_attn with the same arguments (a row whose lse is -infinity adds nothing).  The weights
- *            of a row sum to 1
+ *   lse      in   from sage_cache4_attn with the same arguments (a row whose lse is -infinity adds nothing, one whose lse is
+ *            no number makes its keys' sums NaN).  The weights of a row sum to 1
  *   weights  in   [B,Hkv,width] fp32, or NULL: zeros;  out  out, the same shape, may be weights itself; width >= columns * page.
  *            Slots from lengths[b] on keep their value
  */

@@ -920,7 +920,8 @@ __device__ __forceinline__ void put_sums(const float (&sum)[4], unsigned bad, fl
     }
     to[16 * h + col] = bad >> h & 1 ? 0.0f : mine;
 }
-// a workgroup's sums for the slots [begin, end), of which no query sees those from `seen` on, added to what they had
+// a workgroup's sums for the slots [begin, end), of which no query sees those from `seen` on, added to what they had (which may
+// be where they go)
 __device__ __forceinline__ void add_sums(const float* sums, const float* had, float* to, int begin, int end, int seen) {
     __syncthreads();
     for (int key = begin + threadIdx.x; key < end; key += WAVES * 64)
@@ -931,7 +932,7 @@ __device__ __forceinline__ void add_sums(const float* sums, const float* had, fl
 // At most 16 rows (a decoding step): their operands stay in registers, a wavefront walks tiles of keys, the next one on its way.
 template <int D, int NG>
 __global__ void __launch_bounds__(WAVES * 64, 4) cache4_weights_few_kernel(Cache4 c, CacheQueries q, const float* __restrict__ lse,
-                                                                        const float* __restrict__ weights, float* __restrict__ out, int width, int chunk) {
+                                                                        const float* weights, float* out, int width, int chunk) {
     __shared__ __attribute__((aligned(16))) _Float16 s_ks[WAVES][TILE * NG];
     // (the sums wait here for one pass at the end: stores between the tiles would be waited for with the next tile's loads)
     __shared__ __attribute__((aligned(16))) float s_sum[FEW_CHUNK];
@@ -998,7 +999,7 @@ __global__ void __launch_bounds__(WAVES * 64, 4) cache4_weights_few_kernel(Cache
 // each wavefront makes the operands of 16 of them in LDS, and all use them.
 template <int D, int NG>
 __global__ void __launch_bounds__(WAVES * 64, 2) cache4_weights_kernel(Cache4 c, CacheQueries q, const float* __restrict__ lse,
-                                                                       const float* __restrict__ weights, float* __restrict__ out, int width) {
+                                                                       const float* weights, float* out, int width) {
     __shared__ __attribute__((aligned(16))) _Float16 s_ks[WAVES][TILE * NG];
     __shared__ half8 s_q[WAVES][D / 32][64];
     __shared__ __attribute__((aligned(16))) float s_sum[WAVES * TILE];
@@ -1110,9 +1111,16 @@ AttnPlan plan(int B, int Hq, int Hkv, int Nq, int capacity, int requested) {
 }
 }  // namespace
 
-long long cache4_attn_workgroups(int B, int Hq, int Hkv, int Nq, int capacity, int n_splits) {
+// the merge: few rows of many chunks have a workgroup each
+static bool wide_merge(size_t rows, int n_splits) { return rows <= 2048 && n_splits > 4; }
+
+// of the larger of the call's launches
+long long cache4_attn_workgroups(int B, int Hq, int Hkv, int Nq, int D, int capacity, int n_splits) {
     const AttnPlan p = plan(B, Hq, Hkv, Nq, capacity, n_splits);
-    return (long long)B * Hkv * p.tiles * p.n_splits;
+    const long long attn = (long long)B * Hkv * p.tiles * p.n_splits;
+    if (p.n_splits <= 1) return attn;
+    const long long rows = (long long)B * Hq * Nq, per = wide_merge(rows, p.n_splits) ? 1 : 1024 / D, merge = (rows + per - 1) / per;
+    return attn > merge ? attn : merge;
 }
 
 size_t cache4_attn_workspace(int B, int Hq, int Hkv, int Nq, int D, int capacity, int n_splits) {
@@ -1148,7 +1156,7 @@ hipError_t launch_cache4_attn(const Cache4& c, const CacheQueries& q, void* out,
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess || p.n_splits <= 1) return e;
 #define SAGE_CACHE4_MERGE(D, LANES, BATCH) cache4_merge_kernel<D, LANES, BATCH><<<(unsigned)((rows * (D / 4) * LANES + 255) / 256), 256, 0, st>>>(c, q, out, os, lse, part, part_lse, p.chunk)
-    const bool wide = rows <= 2048 && p.n_splits > 4;
+    const bool wide = wide_merge(rows, p.n_splits);
     if (c.D == 64) { if (wide) SAGE_CACHE4_MERGE(64, 16, 4); else SAGE_CACHE4_MERGE(64, 1, 4); }
     else { if (wide) SAGE_CACHE4_MERGE(128, 8, 4); else SAGE_CACHE4_MERGE(128, 1, 4); }
 #undef SAGE_CACHE4_MERGE

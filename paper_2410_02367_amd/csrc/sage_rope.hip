@@ -101,19 +101,15 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeTensor q, RopeTensor k, c
         }
 }
 
-// Pairs that no vector fits: one thread per pair of channels (and per pair of channels that pass).
+// Pairs that no vector fits: one thread per pair of channels of a head (and per pair of channels that pass).
 template <class T>
 __global__ void __launch_bounds__(256) rope_pair_kernel(RopeTensor q, RopeTensor k, const int* __restrict__ positions, long position_stride,
                                                         const double* __restrict__ inv_freq, float amplitude, int N, int D, int R,
                                                         int interleaved, float sign, long total) {
-    const int pairs = D / 2, H = q.H + k.H;
-    const long w = blockIdx.x * 256l + threadIdx.x;
+    const int pairs = D / 2, h = blockIdx.y;
+    const long w = blockIdx.x * 256l + threadIdx.x, token = w / pairs;
     if (w >= total) return;
-    const int i = (int)(w % pairs);
-    long r = w / pairs;
-    const int h = (int)(r % H);
-    r /= H;
-    const int n = (int)(r % N), b = (int)(r / N);
+    const int i = (int)(w - token * pairs), b = (int)(token / N), n = (int)(token - (long)b * N);
     const RopeTensor& t = h < q.H ? q : k;
     const int ht = h < q.H ? h : h - q.H;
     const T* x = (const T*)t.x + b * t.xs.b + ht * t.xs.h + n * t.xs.n;
@@ -148,9 +144,9 @@ static void launch_rope_type(const RopeTensor& q, const RopeTensor& k, const int
         if (tokens * H * (D / 16) < (1l << 17)) SAGE_ROPE(VEC, 1);
         else SAGE_ROPE(VEC, 4);
     } else {
-        const long total = tokens * H * (D / 2);
-        rope_pair_kernel<T><<<(unsigned)((total + 255) / 256), 256, 0, st>>>(q, k, positions, position_stride, inv_freq, amplitude, N, D, R, interleaved,
-                                                                             sign, total);
+        const long total = tokens * (D / 2);
+        rope_pair_kernel<T><<<dim3((unsigned)((total + 255) / 256), H), 256, 0, st>>>(q, k, positions, position_stride, inv_freq, amplitude, N, D, R,
+                                                                                      interleaved, sign, total);
     }
 #undef SAGE_ROPE
 }

@@ -63,7 +63,7 @@ struct CacheQueries {
     int B, Hq, Nq, type, causal;
     float sm_scale;
 };
-long long cache4_attn_workgroups(int B, int Hq, int Hkv, int Nq, int capacity, int n_splits);
+long long cache4_attn_workgroups(int B, int Hq, int Hkv, int Nq, int D, int capacity, int n_splits);
 size_t cache4_attn_workspace(int B, int Hq, int Hkv, int Nq, int D, int capacity, int n_splits);
 hipError_t launch_cache4_attn(const Cache4& c, const CacheQueries& q, void* out, const RowStrides& os, float* lse, void* workspace,
                               int n_splits, hipStream_t st);

@@ -7,6 +7,9 @@ namespace {
 
 using sage::RowStrides;
 
+// a launch counts its threads, 256 per workgroup here, in 32 bits
+constexpr long long MOST_WORKGROUPS = (1ll << 24) - 1;
+
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 bool fp16_or_bf16(int type) { return type == SAGE_F16 || type == SAGE_BF16; }
 
@@ -65,6 +68,7 @@ int rope(const void* q, const int64_t* q_strides, void* q_out, const int64_t* q_
     if (Hk < 0 || position_stride < 0 || D <= 0) return SAGE_ERR_SHAPE;
     if (int e = check_shape(B, Hq, N)) return e;
     if (int e = check_shape(B, Hq + Hk, N)) return e;
+    if ((long long)B * N * D > 512 * MOST_WORKGROUPS) return SAGE_ERR_SHAPE;         // (a thread per pair of channels)
     if (type != SAGE_F16 && type != SAGE_BF16 && type != SAGE_F32) return SAGE_ERR_UNSUPPORTED;
     if (D % 8 != 0 || D > 512 || rotated < 2 || rotated > D || rotated % 2 != 0) return SAGE_ERR_UNSUPPORTED;
     if (!std::isfinite(amplitude)) return SAGE_ERR_VALUE;
@@ -142,8 +146,7 @@ int sage_cache4_attn(const void* q, const int64_t* q_strides, const void* cache,
     if (int e = check_cache(cache, pages, B, Hkv, D, num_pages, columns, page, group)) return e;
     if (int e = check_queries(B, Hq, Hkv, Nq, type, sm_scale)) return e;
     if (n_splits < 0) return SAGE_ERR_VALUE;
-    // (workgroups are counted in an int by the kernels)
-    if (sage::cache4_attn_workgroups(B, Hq, Hkv, Nq, columns * page, n_splits) > (1ll << 30)) return SAGE_ERR_SHAPE;
+    if (sage::cache4_attn_workgroups(B, Hq, Hkv, Nq, D, columns * page, n_splits) > MOST_WORKGROUPS) return SAGE_ERR_SHAPE;
     const size_t need = sage_cache4_attn_workspace(B, Hq, Hkv, Nq, D, columns, page, n_splits);
     if (need > 0 && !workspace) return SAGE_ERR_NULL;
     if (workspace_bytes < need) return SAGE_ERR_WORKSPACE;

@@ -111,6 +111,8 @@ def sage_rope_frequencies(rotated: int, base: float = 10000.0, scaling: str | No
         raise ValueError("rotated: an even number of channels")
     if not (base > 0 and factor >= 1 and original_length > 0 and 0 < low < high):
         raise ValueError("base and original_length are positive, factor at least 1, 0 < low < high")
+    if scaling == "ramp" and base <= 1:
+        raise ValueError("base: above 1, where the pairs differ in frequency")
     index = torch.arange(0, rotated, 2, dtype=torch.float64)
     if scaling == "base":
         base = base * factor ** (rotated / (rotated - 2)) if rotated > 2 else base

@@ -214,3 +214,23 @@ def test_scaled_frequencies():
                 dict(rotated=64, low=4.0, high=1.0)):
         with pytest.raises(ValueError):
             sage.sage_rope_frequencies(**bad)
+
+
+def test_launches_beyond_what_32_bits_count(lib):
+    """A launch of 2^32 threads and more is refused before anything runs."""
+    def attn(B, Hq, Nq, splits, columns):
+        return lib.sage_cache4_attn(GOOD, None, GOOD, GOOD, GOOD, None, GOOD, None, None, GOOD, 1 << 62, B, Hq, 1, Nq, 64, 0, 1 << 20, columns, 256, 32, 1,
+                                    F(0.125), splits, None)
+    assert attn(1 << 14, 1, 1, 1 << 10, 1 << 10) == 2                   # 2^24 chunks of one row each
+    assert attn(1 << 4, 1 << 10, 1 << 14, 2, 2) == 2                    # 2^28 rows of two chunks: the merge's threads
+    for name in ("sage_rope", "sage_rope_bwd"):
+        for rotated in (64, 2):
+            assert getattr(lib, name)(GOOD, None, GOOD, None, None, None, None, None, GOOD, 0, GOOD, F(1.0), 16, 1, 0, 1 << 23, 64, rotated, 0, 0, None) == 2
+
+
+def test_frequencies_that_are_refused():
+    import paper_2410_02367_amd as sage
+    for bad in (dict(rotated=7), dict(rotated=0), dict(base=0.0), dict(factor=0.5), dict(original_length=0), dict(low=2.0, high=1.0),
+                dict(scaling="other"), dict(scaling="ramp", base=1.0)):
+        with pytest.raises(ValueError):
+            sage.sage_rope_frequencies(**{"rotated": 64, **bad})
