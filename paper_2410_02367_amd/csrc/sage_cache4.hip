@@ -194,25 +194,56 @@ hipError_t launch_cache4_load(const Cache4& c, const int* start, const int* coun
 // ---- eviction
 // The slots that stay, in order: the last `recent` of n and, of the m before them, the need = keep - recent with the largest
 // weights, of equal ones the lowest slots.  One workgroup per (sequence, head); a wavefront has a share of the slots of its
-// own, the first 1024 of them in registers.  The need-th largest weight is found 11, 11 and 10 bits at a time from the top: a
-// histogram of the weights that share the bits found so far, and a sum over the bins from the largest down.  Then every
-// wavefront counts those of its share above it and equal to it, and writes its share.
+// own, the first 1024 of them in registers.  The need-th largest weight is closed in on: [low, high] holds it, at first the smallest and
+// the largest weight; 2048 bins over it are counted, summed from the largest down, and one of them is the next [low, high].  At most
+// 64 weights left are compared each with each.  (Bins over what is there, not over fixed bits: weights of a softmax
+// share most of their upper bits, and one pass leaves a handful: 64 heads of 16K slots 17 us, 12 if all are equal, 25 if most are; by
+// 11, 11 and 10 bits from the top 23.)  Then every wavefront counts those of its share above it and equal
+// to it, and writes its share.
 namespace {
-// larger weight, larger key; a NaN below all numbers, -0 with 0
+// larger weight, larger key; a NaN below all numbers, -0 with 0; 0 is no weight's
 __device__ __forceinline__ unsigned rank_key(float w) {
     const unsigned u = __builtin_bit_cast(unsigned, w + 0.0f);
-    return w != w ? 0u : (u >> 31 ? ~u : u | 0x80000000u);
+    return w != w ? 1u : (u >> 31 ? ~u : u | 0x80000000u);
 }
 __device__ __forceinline__ int popcount(unsigned long long x) { return __builtin_popcountll(x); }
+// bits of x below the lane's own
+__device__ __forceinline__ int before(unsigned long long x) {
+    return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(x >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)x, 0u));
+}
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ unsigned moved(unsigned otherwise, unsigned x) {
+    return (unsigned)__builtin_amdgcn_update_dpp((int)otherwise, (int)x, CTRL, ROWS, 0xF, false);
+}
+// over 16 lanes, in all of them
+template <class F>
+__device__ __forceinline__ unsigned over16(unsigned x, F&& f) {
+    x = f(x, moved<0xB1>(x, x));                // lane ^ 1
+    x = f(x, moved<0x4E>(x, x));                // lane ^ 2
+    x = f(x, moved<0x141>(x, x));               // the other half of 8, mirrored
+    return f(x, moved<0x140>(x, x));            // the other half of 16, mirrored
+}
+// the sum over the lanes up to the own
+__device__ __forceinline__ int running_sum(int x) {
+    x += (int)moved<0x111>(0u, (unsigned)x);            // from the lane 1, 2, 4, 8 before, of 16
+    x += (int)moved<0x112>(0u, (unsigned)x);
+    x += (int)moved<0x114>(0u, (unsigned)x);
+    x += (int)moved<0x118>(0u, (unsigned)x);
+    x += (int)moved<0x142, 0xA>(0u, (unsigned)x);       // the 16 before's last to the second and fourth 16
+    x += (int)moved<0x143, 0xC>(0u, (unsigned)x);       // the first 32's last to the others
+    return x;
+}
 }  // namespace
 
-constexpr int SELECT_NT = 1024, SELECT_WAVES = SELECT_NT / 64, SELECT_HELD = 16, SELECT_BINS = 2048, SELECT_COPIES = 4;
+constexpr int SELECT_NT = 1024, SELECT_WAVES = SELECT_NT / 64, SELECT_HELD = 16, SELECT_BINS = 2 * SELECT_NT, SELECT_COPIES = 4, SELECT_LIST = 64;
+static_assert(SELECT_WAVES == 16 && SELECT_LIST == 64, "a value per wavefront in 16 lanes, a listed weight per lane");
 __global__ void __launch_bounds__(SELECT_NT) cache4_select_kernel(const int* __restrict__ lengths, const float* __restrict__ weights, int width,
                                                                   int capacity, int heads, int* __restrict__ kept,
                                                                   int* __restrict__ out_lengths, int keep, int recent) {
     // (copies, one for every fourth lane: weights of like size fall into few bins, and additions to one word wait for each other)
-    __shared__ int histogram[SELECT_COPIES][SELECT_BINS + 8];
-    __shared__ int s_digit, s_above, s_count, s_total[SELECT_WAVES], s_gt[SELECT_WAVES], s_eq[SELECT_WAVES];
+    __shared__ __attribute__((aligned(16))) int histogram[SELECT_COPIES][SELECT_BINS + 8];
+    __shared__ unsigned s_low[SELECT_WAVES], s_high[SELECT_WAVES], s_list[SELECT_LIST];
+    __shared__ int s_digit, s_above, s_count, s_listed, s_rank[SELECT_LIST], s_total[SELECT_WAVES], s_gt[SELECT_WAVES], s_eq[SELECT_WAVES];
     const int bh = blockIdx.x, b = bh / heads, t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int n = min(max(lengths[b], 0), capacity);
     int* const to = kept + (size_t)bh * keep;
@@ -232,98 +263,123 @@ __global__ void __launch_bounds__(SELECT_NT) cache4_select_kernel(const int* __r
         const int i = first + 64 * j + lane;
         held[j] = i < last ? rank_key(w[i]) : 0u;
     }
-    // f(key, slot, whether there is one) for the lane's slots, 64 neighbouring ones of the wavefront at a time
+    // f(key, slot) for the lane's slots, 64 neighbouring ones of the wavefront at a time; key 0: none there
     auto walk = [&](auto&& f) {
 #pragma unroll
         for (int j = 0; j < SELECT_HELD; ++j)
-            if (first + 64 * j < last) f(held[j], first + 64 * j + lane, first + 64 * j + lane < last);
+            if (first + 64 * j < last) f(held[j], first + 64 * j + lane);
         for (int i0 = first + 64 * SELECT_HELD; i0 < last; i0 += 64 * 4) {
             float x[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[j] = w[min(i0 + 64 * j + lane, m - 1)];
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (i0 + 64 * j < last) f(rank_key(x[j]), i0 + 64 * j + lane, i0 + 64 * j + lane < last);
+                if (i0 + 64 * j < last) f(i0 + 64 * j + lane < last ? rank_key(x[j]) : 0u, i0 + 64 * j + lane);
         }
     };
-    unsigned found = 0, mask = 0;
-    int left = need;                    // of the keys that match `found` under `mask`, how many stay
+    auto smaller = [](unsigned x, unsigned y) { return x < y ? x : y; };
+    auto larger = [](unsigned x, unsigned y) { return x > y ? x : y; };
+    auto sum = [](unsigned x, unsigned y) { return x + y; };
+    // of the wavefronts' values those before this one's, added up
+    auto sum_before = [&](const int* of) { return (int)over16((lane & 15) < wave ? (unsigned)of[lane & 15] : 0u, sum); };
+    typedef int pair_t __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int step = 0; step < 3; ++step) {
-        const int shift = step == 0 ? 21 : step == 1 ? 10 : 0;
-        const unsigned bins = step == 2 ? 1023u : 2047u;
+    for (int i = 0; i < SELECT_COPIES; ++i) *(pair_t*)&histogram[i][2 * t] = (pair_t){0, 0};
+    if (t < SELECT_LIST) s_rank[t] = 0;
+    if (t == 0) s_listed = 0;
+    unsigned low = ~0u, high = 0u;
+    walk([&](unsigned u, int) {
+        low = smaller(low, u - 1u);
+        high = larger(high, u);
+    });
+    low = over16(low, smaller);
+    high = over16(high, larger);
+    low = smaller(low, __shfl_xor(low, 16, 64));
+    high = larger(high, __shfl_xor(high, 16, 64));
+    low = smaller(low, __shfl_xor(low, 32, 64));
+    high = larger(high, __shfl_xor(high, 32, 64));
+    if (lane == 0) {
+        s_low[wave] = low;
+        s_high[wave] = high;
+    }
+    __syncthreads();
+    low = __builtin_amdgcn_readfirstlane(over16(s_low[lane & 15], smaller)) + 1u;
+    high = __builtin_amdgcn_readfirstlane(over16(s_high[lane & 15], larger));
+    int left = need, count = m;         // of the `count` keys in [low, high], how many stay
+    while (left < count && low < high) {
+        const unsigned span = high - low;
+        if (count <= SELECT_LIST) {
+            walk([&](unsigned u, int) {
+                if (u - low <= span) s_list[atomicAdd(&s_listed, 1)] = u;
+            });
+            __syncthreads();
+            const unsigned x = lane < count ? s_list[lane] : 0u;
+            int rank = 0;               // larger ones, and 2^16 times the equal ones
 #pragma unroll
-        for (int i = 0; i < SELECT_COPIES; ++i) histogram[i][t] = histogram[i][t + SELECT_NT] = 0;
-        __syncthreads();
-        walk([&](unsigned u, int, bool is) {
-            const bool counts = is && (u & mask) == found;
-            const unsigned long long all = __builtin_amdgcn_ballot_w64(counts);
-            if (all == 0) return;
-            // equal keys are common (zeros): one addition for the wavefront
-            const unsigned d = u >> shift & bins, one = __builtin_amdgcn_readlane(d, __builtin_ctzll(all));
-            if (__builtin_amdgcn_ballot_w64(counts && d != one) == 0) {
-                if (lane == 0) atomicAdd(&histogram[0][one], popcount(all));
-            } else if (counts) {
-                atomicAdd(&histogram[lane % SELECT_COPIES][d], 1);
+            for (int i = 0; i < SELECT_LIST / SELECT_WAVES; ++i) {
+                const int at = wave * (SELECT_LIST / SELECT_WAVES) + i;
+                const unsigned y = at < count ? __builtin_amdgcn_readlane(x, at) : 0u;
+                rank += y > x ? 1 : y == x ? 1 << 16 : 0;
             }
-        });
-        __syncthreads();
-        // thread t: bins 2 t and 2 t + 1; `above`: keys in the bins after them
-        int h0 = 0, h1 = 0;
-#pragma unroll
-        for (int i = 0; i < SELECT_COPIES; ++i) {
-            h0 += histogram[i][2 * t];
-            h1 += histogram[i][2 * t + 1];
-        }
-        int above = h0 + h1;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int x = __shfl_down(above, off, 64);
-            above += lane + off < 64 ? x : 0;
-        }
-        if (lane == 0) s_total[wave] = above;
-        __syncthreads();
-        above -= h0 + h1;
-        for (int i = wave + 1; i < SELECT_WAVES; ++i) above += s_total[i];
-        if (above < left && left <= above + h1) {
-            s_digit = 2 * t + 1;
-            s_above = above;
-            s_count = h1;
-        } else if (above + h1 < left && left <= above + h1 + h0) {
-            s_digit = 2 * t;
-            s_above = above + h1;
-            s_count = h0;
-        }
-        __syncthreads();
-        found |= (unsigned)s_digit << shift;
-        mask |= bins << shift;
-        left -= s_above;
-        if (left == s_count) {          // all keys with these bits stay: whatever the others are, from 0 on
-            left = m;
+            atomicAdd(&s_rank[lane], rank);
+            __syncthreads();
+            rank = s_rank[lane];
+            const int above = rank & 0xffff, equal = rank >> 16;
+            const int one = __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < count && above < left && left <= above + equal));
+            low = __builtin_amdgcn_readlane(x, one);
+            left -= __builtin_amdgcn_readlane(above, one);
+            count = __builtin_amdgcn_readlane(equal, one);
             break;
         }
+        const int shift = max(21 - (int)__builtin_clz(span), 0);
+        walk([&](unsigned u, int) {
+            const unsigned d = u - low;
+            if (d <= span) atomicAdd(&histogram[lane % SELECT_COPIES][d >> shift], 1);
+        });
+        __syncthreads();
+        // thread t: two bins, from the largest down; `above`: keys in the bins before them
+        const int bin = SELECT_BINS - 2 - 2 * t;
+        pair_t h = {0, 0};
+#pragma unroll
+        for (int i = 0; i < SELECT_COPIES; ++i) {
+            h += *(const pair_t*)&histogram[i][bin];
+            *(pair_t*)&histogram[i][bin] = (pair_t){0, 0};
+        }
+        int above = running_sum(h[0] + h[1]);
+        if (lane == 63) s_total[wave] = above;
+        __syncthreads();
+        above += sum_before(s_total) - h[0] - h[1];
+        if (above < left && left <= above + h[0] + h[1]) {
+            const bool upper = left <= above + h[1];
+            s_digit = upper ? bin + 1 : bin;
+            s_above = upper ? above : above + h[1];
+            s_count = upper ? h[1] : h[0];
+        }
+        __syncthreads();
+        low += (unsigned)__builtin_amdgcn_readfirstlane(s_digit) << shift;
+        high = smaller(high, low + ((1u << shift) - 1u));
+        left -= __builtin_amdgcn_readfirstlane(s_above);
+        count = __builtin_amdgcn_readfirstlane(s_count);
     }
+    const unsigned found = low;
+    if (left == count) left = m;        // all keys in [low, high] stay: whatever is there from low on
     int gt = 0, eq = 0;
-    walk([&](unsigned u, int, bool is) {
-        gt += popcount(__builtin_amdgcn_ballot_w64(is && u > found));
-        eq += popcount(__builtin_amdgcn_ballot_w64(is && u == found));
+    walk([&](unsigned u, int) {
+        gt += popcount(__builtin_amdgcn_ballot_w64(u > found));
+        eq += popcount(__builtin_amdgcn_ballot_w64(u == found));
     });
     if (lane == 0) {
         s_gt[wave] = gt;
         s_eq[wave] = eq;
     }
     __syncthreads();
-    int at = 0, ties = 0;               // slots written, equal ones seen before this share
-    for (int i = 0; i < wave; ++i) {
-        at += s_gt[i];
-        ties += s_eq[i];
-    }
-    at += min(ties, left);
-    walk([&](unsigned u, int i, bool is) {
-        const unsigned long long equal = __builtin_amdgcn_ballot_w64(is && u == found), below = (1ull << lane) - 1ull;
-        const bool stays = is && (u > found || (u == found && ties + popcount(equal & below) < left));
+    int ties = __builtin_amdgcn_readfirstlane(sum_before(s_eq));        // equal ones before this share
+    int at = __builtin_amdgcn_readfirstlane(sum_before(s_gt)) + min(ties, left);
+    walk([&](unsigned u, int i) {
+        const unsigned long long equal = __builtin_amdgcn_ballot_w64(u == found);
+        const bool stays = u > found || (u == found && ties + before(equal) < left);
         const unsigned long long all = __builtin_amdgcn_ballot_w64(stays);
-        if (stays) to[at + popcount(all & below)] = i;
+        if (stays) to[at + before(all)] = i;
         at += popcount(all);
         ties += popcount(equal);
     });

@@ -85,3 +85,24 @@ def test_into_another_pool_and_long():
     at = dev(want)
     for x, y in zip(a, b):
         assert torch.equal(x[:, :, at].view(torch.int16), y.view(torch.int16))
+
+
+def bits(low, high):
+    """Weights whose bit patterns are evenly spread: as many powers of two as there are."""
+    return lambda g, s: g.integers(low, high, s, dtype=np.uint32).view(np.float32)
+
+
+@pytest.mark.parametrize("weights", [bits(0, 0x7f800000), bits(0x3f800000, 0x3f800800), bits(0x3f800000, 0x3f800801), bits(0x3f800000, 0x3f800002),
+                                     lambda g, s: np.where(g.random(s) < 0.9, 1.0, g.random(s)).astype(np.float32),
+                                     lambda g, s: np.where(g.random(s) < 0.97, 2.0 ** -100, np.repeat(g.random((*s[:2], 1)), s[2], 2)).astype(np.float32),
+                                     lambda g, s: np.where(g.random(s) < 0.01, np.inf, 1.0 + g.integers(0, 90, s) * 2.0 ** -23).astype(np.float32)],
+                         ids=["all", "2048", "2049", "two", "mostly one", "mostly the least", "neighbours"])
+@pytest.mark.parametrize("keep", [9, 65, 700, 1090])
+def test_weights_that_are_alike(weights, keep):
+    case(keep, 2, 2, 64, 16, 32, [1100, 1095], keep, 8, weights)
+
+
+def test_many_alike_beyond_the_registers():
+    # one key in 1000 differs; 40000 of them
+    case(7, 1, 1, 64, 256, 64, [40000], 39950, 3, lambda g, s: np.where(g.random(s) < 1e-3, g.random(s), 0.5).astype(np.float32))
+    case(8, 1, 1, 64, 256, 64, [40000], 60, 3, bits(0x3f800000, 0x40000000))
