@@ -378,16 +378,30 @@ def check_no_spills(text: str) -> list:
     return problems
 
 
+def check_cache4_attn_asm(text: str) -> list:
+    """The kernels over the 4-bit cache: no scratch access between a kernel's first matrix instruction and its last, which is the
+    walk over the keys (at its head the kernel with 32 rows and four scales per key reads two addresses back)."""
+    import re
+    problems = []
+    for m in re.finditer(r"^(_ZN4sage\w+):.*?^\.Lfunc_end\d+:", text, re.S | re.M):
+        lines = m.group(0).split("\n")
+        products = [i for i, line in enumerate(lines) if "v_mfma" in line]
+        walk = lines[products[0]:products[-1]] if products else lines
+        if any("scratch_" in line for line in walk):
+            problems.append(f"{m.group(1)}: scratch access (register spill)")
+    return problems
+
+
 def verify_attention_isa(extra=()) -> None:
-    """Compiles the kernel sources to assembly and raises RuntimeError if check_attention_asm(),
-    check_loads_asm() or check_no_spills() objects."""
+    """Compiles the kernel sources to assembly and raises RuntimeError if one of the checks above objects."""
     import tempfile
     flags = [f for f in HIPCC_FLAGS if f not in ("-shared", "-fPIC")]
     problems = []
     with tempfile.TemporaryDirectory() as tmp:
         for src, check in (("sage_attn.hip", lambda s: check_attention_asm(s) + check_attention_registers(s) + check_two_sets(s)), ("sage_attn_pv8.hip", check_pv8_asm),
                            ("sage_prepass.hip", check_no_spills), ("sage_prepass_v.hip", check_no_spills),
-                           ("sage_short.hip", check_short_asm), ("sage_short.hip", check_short_pair_asm), ("sage_decode.hip", check_decode_asm)):
+                           ("sage_short.hip", check_short_asm), ("sage_short.hip", check_short_pair_asm), ("sage_decode.hip", check_decode_asm),
+                           ("sage_rope.hip", check_no_spills), ("sage_cache4.hip", check_no_spills), ("sage_cache4_attn.hip", check_cache4_attn_asm)):
             out = os.path.join(tmp, src + ".s")
             cmd = [hipcc(), *flags, *extra, "-S", "--cuda-device-only", "-o", out, os.path.join(CSRC, src)]
             res = subprocess.run(cmd, capture_output=True, text=True)

@@ -217,3 +217,15 @@ def test_source_hash_guard_tells_a_foreign_binary_from_ours(tmp_path):
     from paper_2410_02367_amd import binding
     binding.load()
     assert not build.is_stale() and binding.sage_source_hash() == h
+
+
+def test_spills_among_the_products():
+    """The walk over the keys of the 4-bit cache: scratch accesses before its first product pass, among the products they do not."""
+    from paper_2410_02367_amd.build import check_cache4_attn_asm
+    kernel = "_ZN4sage18cache4_attn_kernelILi%dE:\n%s\n\tv_mfma_f32_16x16x32_f16 a\n%s\n\tv_mfma_f32_16x16x32_f16 b\n\ts_endpgm\n.Lfunc_end%d:\n"
+    clean = kernel % (64, "\tscratch_store_dword off, v1, off", "\tv_add_f32 v0, v1, v2", 0)
+    assert check_cache4_attn_asm(clean) == []
+    problems = check_cache4_attn_asm(clean + kernel % (128, "", "\tscratch_load_dword v1, off, off", 1))
+    assert len(problems) == 1 and "ILi128E" in problems[0]
+    merge = "_ZN4sage19cache4_merge_kernelILi64E:\n\tscratch_load_dword v1, off, off\n.Lfunc_end2:\n"
+    assert len(check_cache4_attn_asm(clean + merge)) == 1
