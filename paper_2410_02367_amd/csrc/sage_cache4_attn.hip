@@ -75,27 +75,34 @@ struct RowRange {
 // -> what turns a scaled sum into the exponent of 2.
 template <int D>
 struct Queries4 {
+    c4u raw[D / 32];
     half8 op[D / 32];
+    __device__ __forceinline__ void request(const CacheQueries& q, long at, int h) {
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) raw[i] = *(const c4u*)((const unsigned short*)q.q + at + 32 * i + 8 * h);
+    }
     __device__ __forceinline__ float load(const CacheQueries& q, long at, int h) {
+        request(q, at, h);
+        return convert(q);
+    }
+    __device__ __forceinline__ float convert(const CacheQueries& q) {
         float x[D / 32][8], m = 0.0f;
         if (q.type == TYPE_F16) {
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) {
-                const half8 v = *(const half8*)((const _Float16*)q.q + at + 32 * i + 8 * h);
+                const half8 v = __builtin_bit_cast(half8, raw[i]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[i][e] = (float)v[e];
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                const c4u v = *(const c4u*)((const unsigned short*)q.q + at + 32 * i + 8 * h);
+            for (int i = 0; i < D / 32; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const unsigned w = v[e];
+                    const unsigned w = raw[i][e];
                     x[i][2 * e] = word_f32(w << 16);
                     x[i][2 * e + 1] = word_f32(w & 0xffff0000u);
                 }
-            }
         }
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
@@ -875,6 +882,22 @@ struct LaneRows {
     float sc[4], reference[4];
     int end[4];
 };
+// 16 rows from `first` on, on their way: queries, lse, slots seen by row lane % 16; of those behind the last the last one's query, which sees
+// none here
+template <int D>
+struct SomeRows {
+    Queries4<D> query;
+    float lse;
+    int end;
+    __device__ __forceinline__ void request(const Cache4& c, const CacheQueries& q, const float* from, const RowRange& range, int b, int head, int first,
+                                            int lane) {
+        const int share = q.Hq / c.heads, at = first + (lane & 15), row = min(at, range.rows - 1), tq = row / share, g = row - tq * share;
+        query.request(q, b * q.strides.b + (head * share + g) * q.strides.h + tq * q.strides.n, lane >> 4);
+        lse = from[((size_t)b * q.Hq + head * share + g) * q.Nq + tq];
+        end = at < range.rows ? range.end(tq, q.causal) : 0;
+    }
+    __device__ __forceinline__ float reference() const { return end > 0 ? row_reference(lse) : __builtin_inff(); }
+};
 template <int NG> using LaneScales = unsigned[(NG + 1) / 2];
 // -> the weights that 16 rows give to the lane's key, rows 4 h .. 4 h + 3 of them; key: the slot.  whole: every row sees it
 template <int D, int NG>
@@ -1033,19 +1056,21 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache4_weights_kernel(Cache4 c,
         // the first row that sees a key of the workgroup
         int row0 = 0;
         if (q.causal) row0 = max(0, k_first + 1 - (range.length - range.count + 1)) * share / 64 * 64;
+        SomeRows<D> some;
+        some.request(c, q, lse, range, b, head, row0 + 16 * wave, lane);
         for (; row0 < range.rows; row0 += 64) {
             {
-                const int at = row0 + 16 * wave + col, row = min(at, range.rows - 1), tq = row / share, g = row - tq * share;
-                Queries4<D> query;
-                const float sc = query.load(q, b * q.strides.b + (head * share + g) * q.strides.h + tq * q.strides.n, h);
+                const float sc = some.query.convert(q), reference = some.reference();
+                const int end = some.end;
                 __syncthreads();                // the rows before have been read
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) s_q[wave][i][lane] = query.op[i];
+                for (int i = 0; i < D / 32; ++i) s_q[wave][i][lane] = some.query.op[i];
                 if (h == 0) {
                     s_sc[wave][col] = sc;
-                    s_reference[wave][col] = at < range.rows ? row_reference(lse[((size_t)b * q.Hq + head * share + g) * q.Nq + tq]) : __builtin_inff();
-                    s_end[wave][col] = at < range.rows ? range.end(tq, q.causal) : 0;
+                    s_reference[wave][col] = reference;
+                    s_end[wave][col] = end;
                 }
+                some.request(c, q, lse, range, b, head, row0 + 64 + 16 * wave, lane);
                 __syncthreads();
             }
 #pragma unroll 1
@@ -1071,6 +1096,74 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache4_weights_kernel(Cache4 c,
     put_sums(sum, bad, s_sum + wave * TILE, lane);
     add_sums(s_sum, weights != nullptr ? weights + (size_t)slab * width : nullptr, out + (size_t)slab * width, k_first, min(k_first + WAVES * TILE, width),
              last_end);
+}
+
+// More rows where 256 keys at a time would leave the chip idle: a workgroup takes 64 keys, whose operands each of its NW wavefronts has
+// in its registers, and a wavefront every NW-th 16 rows; the sums of a key are added in the wavefronts' order.  The price: the
+// rows' operands are made for 64 keys instead of for 256.
+template <int D, int NG, int NW>
+__global__ void __launch_bounds__(NW * 64, 2) cache4_weights_rows_kernel(Cache4 c, CacheQueries q, const float* __restrict__ lse,
+                                                                            const float* weights, float* out, int width) {
+    __shared__ __attribute__((aligned(16))) _Float16 s_ks[NW][TILE * NG];
+    __shared__ __attribute__((aligned(16))) float s_sum[NW][TILE];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
+    const int slab = blockIdx.y, b = slab / c.heads, head = slab - b * c.heads, share = q.Hq / c.heads;
+    const RowRange range(c, q, b, share);
+    const int last_end = range.rows > 0 ? range.end(range.count - 1, q.causal) : 0, k0 = blockIdx.x * TILE;
+    float sum[4] = {};
+    unsigned bad = 0;
+    int row0 = 16 * wave;
+    // (of the first rows those that see no key of the workgroup are passed over)
+    if (q.causal) row0 += max(0, k0 + 1 - (range.length - range.count + 1)) * share / (16 * NW) * (16 * NW);
+    if (k0 < last_end && row0 < range.rows) {
+        half8 k[4][D / 32];
+        LaneScales<NG> ks[4];
+        {
+            PageIds pages;
+            pages.look_up(c, c.table + (size_t)b * c.columns, k0);
+            KeyTile<D, NG, false> tile;
+            tile.request(c, c.data + (size_t)head * c.block_bytes, pages, k0, lane);
+            *(typename ScaleWord<NG>::type*)(s_ks[wave] + lane * NG) = tile.ks;
+            bad = tile.bad;
+            wave_order();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                lane_scales<NG>(s_ks[wave], 16 * j + col, ks[j]);
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) k[j][i] = operand(tile.k[j][i]);
+            }
+        }
+        SomeRows<D> some;
+        some.request(c, q, lse, range, b, head, row0, lane);
+        for (; row0 < range.rows; row0 += 16 * NW) {
+            const float sc = some.query.convert(q), reference = some.reference();
+            const int end = some.end, first_end = range.end(row0 / share, q.causal);
+            half8 op[D / 32];
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) op[i] = some.query.op[i];
+            some.request(c, q, lse, range, b, head, row0 + 16 * NW, lane);
+            LaneRows rows;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                rows.sc[r] = __shfl(sc, 4 * h + r, 64);
+                rows.reference[r] = __shfl(reference, 4 * h + r, 64);
+                rows.end[r] = __shfl(end, 4 * h + r, 64);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                sum[j] += piece_weights<D, NG>(op, k[j], ks[j], rows, k0 + 16 * j + col, k0 + TILE <= first_end);
+        }
+    }
+    put_sums(sum, bad, s_sum[wave], lane);
+    __syncthreads();
+    const int key = k0 + lane;
+    if (wave != 0 || key >= width) return;
+    float* const to = out + (size_t)slab * width;
+    const float had = weights != nullptr ? weights[(size_t)slab * width + key] : 0.0f;
+    float x = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) x += s_sum[w][lane];
+    to[key] = had + (key < last_end ? x : 0.0f);
 }
 
 namespace {
@@ -1163,19 +1256,27 @@ hipError_t launch_cache4_attn(const Cache4& c, const CacheQueries& q, void* out,
     return hipGetLastError();
 }
 
+// 64 keys per workgroup where 256 would make fewer workgroups than there are compute units and the rows are several rounds of 64 (us with 64 /
+// 256 keys: 828 rows of 12 slabs of 338 keys 10 / 34, 197 of 48 of 777 10 / 12, 512 of 16 of 2048 17 / 24; not 128 of 16 of 4096, 16 / 9,
+// nor 48 of 8 of 4096, 7 / 6); 8 wavefronts where those are few as well (8192 rows of one slab of 16K: 4 / 8 wavefronts 150 / 102, 828
+// of 12 of 338 15 / 10; not 512 of 16 of 2048, 17 / 19).
+constexpr int NARROW = 256;
 hipError_t launch_cache4_weights(const Cache4& c, const CacheQueries& q, const float* lse, const float* weights, float* out, int width,
                                  hipStream_t st) {
     const int slabs = q.B * c.heads, ng = c.groups, tiles = (width + WAVES * TILE - 1) / (WAVES * TILE);
     const bool few = q.Hq / c.heads * q.Nq <= 16;
+    const bool narrow = (long)tiles * slabs < NARROW && q.Hq / c.heads * q.Nq > 64, eight = (long)tiles * slabs <= NARROW / 4;
     // few rows: as many workgroups as the attention has, so that a wavefront has tiles to walk
     int chunks = few ? WANTED_FEW / slabs : tiles;
     if (chunks < 1) chunks = 1;
     if (chunks > tiles) chunks = tiles;
     const int longest = few ? FEW_CHUNK : WAVES * TILE, even = (tiles + chunks - 1) / chunks * WAVES * TILE, chunk = even < longest ? even : longest;
-    const dim3 grid((width + chunk - 1) / chunk, slabs);
+    const dim3 grid((width + chunk - 1) / chunk, slabs), by_64((width + TILE - 1) / TILE, slabs);
 #define SAGE_CACHE4_WEIGHTS(D, NG)                                                                                          \
     do {                                                                                                                     \
         if (few) cache4_weights_few_kernel<D, NG><<<grid, WAVES * 64, 0, st>>>(c, q, lse, weights, out, width, chunk);        \
+        else if (narrow && eight) cache4_weights_rows_kernel<D, NG, 8><<<by_64, 8 * 64, 0, st>>>(c, q, lse, weights, out, width); \
+        else if (narrow) cache4_weights_rows_kernel<D, NG, 4><<<by_64, 4 * 64, 0, st>>>(c, q, lse, weights, out, width);      \
         else cache4_weights_kernel<D, NG><<<grid, WAVES * 64, 0, st>>>(c, q, lse, weights, out, width);                       \
     } while (0)
     if (c.D == 64 && ng == 1) SAGE_CACHE4_WEIGHTS(64, 1);

@@ -100,6 +100,20 @@ def test_many_rows_pages_that_are_none_and_several_chunks(causal):
     case(24, 2, 4, 2, 80, 64, 16, 64, "bf16", [90, 85], extra=128, n_splits=1, q_gain=25.0, causal=causal, weights=False)
 
 
+# tables with room for 1K, 8K and 16K tokens: 64 keys per workgroup with 8 or 4 wavefronts, and 256 keys
+@pytest.mark.parametrize("room", [1024, 8192, 16384])
+@pytest.mark.parametrize("D,group,page", FORMS)
+@pytest.mark.parametrize("Hq,Hkv,Nq,lengths,count,causal", [(2, 2, 65, [65, 300], None, True), (6, 2, 41, [200, 20], [41, 30], True),
+                                                           (2, 2, 150, [70, 333], [149, 3], False), (14, 2, 30, [1, 129], [30, 0], True)])
+def test_weights_of_many_rows(Hq, Hkv, Nq, lengths, count, causal, D, group, page, room):
+    case(Nq + page, 2, Hq, Hkv, Nq, D, page, group, "bf16", lengths, count, causal, extra=room // page)
+
+
+@pytest.mark.parametrize("room", [1024, 8192, 16384])
+def test_weights_of_many_rows_with_pages_that_are_none(room):
+    case(31, 2, 4, 2, 60, 64, 16, 32, "f16", [150, 64], bad=[(0, 0), (0, 4), (1, 3), (1, 2)], extra=room // 16)
+
+
 def test_lengths_beyond_the_table_and_below_zero():
     case(8, 3, 2, 2, 3, 64, 16, 64, "f16", [40, 7, 33], count=[5, -1, 3])
     import paper_2410_02367_amd as sage
