@@ -1169,15 +1169,20 @@ __global__ void __launch_bounds__(NW * 64, 2) cache4_weights_rows_kernel(Cache4 
 namespace {
 // How a call is cut.  Keys: chunks of a multiple of 256, as many as it takes to have WANTED workgroups, two per compute unit (us with
 // 256 / 512 / 1024 workgroups: 256 slabs of 16K keys 146 / 112 / 110, 8 of 128K 40 / 36 / 40, 64 of 16K with 64 rows 110 / 90 / 98), none
-// shorter than 512 unless the caller asks for it.  Sequences of a batch differ in length: up to four times as many chunks of 2048 keys
-// even that out (256 slabs of 8K to 16K keys: 2 chunks 117, 8 chunks 106; all of 16K: 126 and 122).  Rows: 16 or 32 per workgroup, whose wavefronts share the keys; or 128, whose
+// shorter than 512 unless the caller asks for it or even those are fewer than the compute units (512 / 256: 20 slabs of 2.4K 14.8 / 13.1, 8 of
+// 16K 15.3 / 13.4; but 6 of 24K, 276 of them, 16.7 / 17.3), and none at all where the walk is shorter than the merge's launch (one chunk /
+// the best cut, 2 slabs: 768 keys of 128 channels 10.0 / 10.4, 1024 11.8 / 10.1; 1280 of 64 channels 9.8 / 10.1, 2048 13.2 / 10.0).  Sequences of a batch differ in length: up to four times as many chunks, of
+// 2048 keys at least, even that out (256 slabs of 8K to 16K keys: 2 chunks 117, 8 chunks 106; all of 16K: 126 and 122; 80 of 18K to 36K
+// with 52 rows: 3 chunks 238, 12 chunks 190; 32 of 16K to 32K with 1024 rows: 2 chunks 729, 8 chunks 646; 16 of 8K to 16K with
+// 1024 rows: 4 chunks 195, 8 chunks 201).  Rows: 16 or 32 per workgroup, whose wavefronts share the keys; or 128, whose
 // wavefronts share the operands, where there are that many and the chunks are long (us with 32 / 128: 4096 rows of 8 slabs of 32K
 // keys 1117 / 934, of 4K 117 / 111, 128 rows of 64 slabs of 16K 125 / 108; chunks of 512 keys: 512 rows of 32 slabs of 2K 42 / 49).
 struct AttnPlan {
     int rows, tiles, n_splits, chunk;       // rows of a workgroup
 };
-constexpr int WANTED = 512, WANTED_FEW = 1024, MANY_ROWS = 128, LONG_CHUNK = 2048;
-AttnPlan plan(int B, int Hq, int Hkv, int Nq, int capacity, int requested) {
+constexpr long UNCUT = 768 * 128 * 16;
+constexpr int COMPUTE_UNITS = 256, WANTED = 512, WANTED_FEW = 1024, MANY_ROWS = 128, LONG_CHUNK = 2048;
+AttnPlan plan(int B, int Hq, int Hkv, int Nq, int D, int capacity, int requested) {
     const int rows = Hq / Hkv * Nq;
     auto cut = [&](int per) {
         AttnPlan p;
@@ -1185,13 +1190,13 @@ AttnPlan plan(int B, int Hq, int Hkv, int Nq, int capacity, int requested) {
         p.tiles = (rows + per - 1) / per;
         const long groups = (long)B * Hkv * p.tiles;
         long n = requested > 0 ? requested : WANTED / groups;
-        const int least = requested > 0 ? 256 : 512;
+        const int least = requested > 0 || groups * (capacity / 512) < COMPUTE_UNITS ? 256 : 512;
         if (n > capacity / least) n = capacity / least;
-        if (requested == 0 && B > 1 && p.tiles == 1) {
+        if (requested == 0 && B > 1) {
             const long more = 4 * WANTED / groups, most = capacity / LONG_CHUNK;
             n = n > more || n > most ? n : more < most ? more : most;
         }
-        if (n < 1) n = 1;
+        if (n < 1 || (requested == 0 && (long)capacity * D * per <= UNCUT)) n = 1;
         p.chunk = (int)(((capacity + n - 1) / n + 255) / 256 * 256);
         p.n_splits = (capacity + p.chunk - 1) / p.chunk;
         return p;
@@ -1209,7 +1214,7 @@ static bool wide_merge(size_t rows, int n_splits) { return rows <= 2048 && n_spl
 
 // of the larger of the call's launches
 long long cache4_attn_workgroups(int B, int Hq, int Hkv, int Nq, int D, int capacity, int n_splits) {
-    const AttnPlan p = plan(B, Hq, Hkv, Nq, capacity, n_splits);
+    const AttnPlan p = plan(B, Hq, Hkv, Nq, D, capacity, n_splits);
     const long long attn = (long long)B * Hkv * p.tiles * p.n_splits;
     if (p.n_splits <= 1) return attn;
     const long long rows = (long long)B * Hq * Nq, per = wide_merge(rows, p.n_splits) ? 1 : 1024 / D, merge = (rows + per - 1) / per;
@@ -1217,7 +1222,7 @@ long long cache4_attn_workgroups(int B, int Hq, int Hkv, int Nq, int D, int capa
 }
 
 size_t cache4_attn_workspace(int B, int Hq, int Hkv, int Nq, int D, int capacity, int n_splits) {
-    const AttnPlan p = plan(B, Hq, Hkv, Nq, capacity, n_splits);
+    const AttnPlan p = plan(B, Hq, Hkv, Nq, D, capacity, n_splits);
     return p.n_splits <= 1 ? 0 : (size_t)p.n_splits * B * Hq * Nq * (D + 1) * sizeof(float);
 }
 
@@ -1234,7 +1239,7 @@ static void launch_attn_form(const AttnPlan& p, const Cache4& c, const CacheQuer
 
 hipError_t launch_cache4_attn(const Cache4& c, const CacheQueries& q, void* out, const RowStrides& os, float* lse, void* workspace,
                               int n_splits, hipStream_t st) {
-    const AttnPlan p = plan(q.B, q.Hq, c.heads, q.Nq, c.capacity(), n_splits);
+    const AttnPlan p = plan(q.B, q.Hq, c.heads, q.Nq, c.D, c.capacity(), n_splits);
     const size_t rows = (size_t)q.B * q.Hq * q.Nq;
     float* const part = p.n_splits > 1 ? (float*)workspace : nullptr;
     float* const part_lse = p.n_splits > 1 ? part + p.n_splits * rows * c.D : nullptr;
