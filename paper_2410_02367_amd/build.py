@@ -379,8 +379,9 @@ def check_no_spills(text: str) -> list:
 
 
 def check_cache4_attn_asm(text: str) -> list:
-    """The kernels over the 4-bit cache: no scratch access between a kernel's first matrix instruction and its last, which is the
-    walk over the keys (at its head the kernel with 32 rows and four scales per key reads two addresses back)."""
+    """The kernels over the 4-bit cache, between a kernel's first matrix instruction and its last, which is the walk over the keys: no
+    scratch access (at the walk's head the kernel with 32 rows and four scales per key reads two addresses back), and no line
+    of inline assembly, whose registers the compiler would not keep apart from those of a matrix instruction still under way."""
     import re
     problems = []
     for m in re.finditer(r"^(_ZN4sage\w+):.*?^\.Lfunc_end\d+:", text, re.S | re.M):
@@ -389,6 +390,9 @@ def check_cache4_attn_asm(text: str) -> list:
         walk = lines[products[0]:products[-1]] if products else lines
         if any("scratch_" in line for line in walk):
             problems.append(f"{m.group(1)}: scratch access (register spill)")
+        written = "\n".join(line for line in walk if line.strip())
+        if any(block.strip() for block in re.findall(r";;#ASMSTART\n(.*?);;#ASMEND", written, re.S)):
+            problems.append(f"{m.group(1)}: inline assembly among matrix instructions")
     return problems
 
 

@@ -41,18 +41,19 @@ constexpr int TILE = 64, WAVES = 4, FEW_CHUNK = 2048;
 // low mantissa bits of 1024 is 1024 + nibble (or + 16 nibble); the packed subtraction is exact and leaves a small whole number.
 // (The nibbles as subnormal numbers would need no exponent and, with the 8 in the other terms, no subtraction: 9 -> 5
 // instructions.  But the matrix pipe aligns a subnormal operand's products as if it were 2^-14, which costs the sums 7 bits.)
-// (Written as one instruction because the compiler takes two for constants that are both scalar.)
-__device__ __forceinline__ unsigned and_or(unsigned w, unsigned mask, unsigned bits) {
-    unsigned d;
-    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(d) : "v"(w), "s"(mask), "v"(bits));
-    return d;
+// (No inline assembly beside matrix instructions: the compiler keeps no distance between one's registers and what such a line writes.
+// An AND and an OR with two scalar constants are two instructions, so that one constant comes from a register, out of its sight.)
+__device__ __forceinline__ unsigned thousands() {
+    unsigned x;
+    asm volatile("v_mov_b32 %0, 0x64006400" : "=v"(x));
+    return x;
 }
-__device__ __forceinline__ half8 operand(unsigned w) {
+__device__ __forceinline__ half8 operand(unsigned w, unsigned thousand) {
     typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-    const unsigned x = w >> 8, thousand = 0x64006400u;
+    const unsigned x = w >> 8;
     const h2 even = {(_Float16)1032.0f, (_Float16)1032.0f}, odd = {(_Float16)1152.0f, (_Float16)1152.0f};
-    const h2 a = __builtin_bit_cast(h2, and_or(w, 0x000f000fu, thousand)) - even, b = __builtin_bit_cast(h2, and_or(w, 0x00f000f0u, thousand)) - odd;
-    const h2 c = __builtin_bit_cast(h2, and_or(x, 0x000f000fu, thousand)) - even, d = __builtin_bit_cast(h2, and_or(x, 0x00f000f0u, thousand)) - odd;
+    const h2 a = __builtin_bit_cast(h2, (w & 0x000f000fu) | thousand) - even, b = __builtin_bit_cast(h2, (w & 0x00f000f0u) | thousand) - odd;
+    const h2 c = __builtin_bit_cast(h2, (x & 0x000f000fu) | thousand) - even, d = __builtin_bit_cast(h2, (x & 0x00f000f0u) | thousand) - odd;
     return (half8){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
@@ -227,9 +228,9 @@ template <int D> __device__ __forceinline__ int v_chunk(int key, int chunk) {
 
 // the larger of three, of both halves (a NaN stays)
 __device__ __forceinline__ unsigned max3_pairs(unsigned a, unsigned b, unsigned c) {
-    unsigned d;
-    asm("v_pk_maximum3_f16 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
-    return d;
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned, __builtin_elementwise_maximum(__builtin_elementwise_maximum(__builtin_bit_cast(h2, a), __builtin_bit_cast(h2, b)),
+                                                                      __builtin_bit_cast(h2, c)));
 }
 __device__ __forceinline__ _Float16 half_of(unsigned w, int hi) { return __builtin_bit_cast(_Float16, (unsigned short)(hi ? w >> 16 : w)); }
 
@@ -377,7 +378,7 @@ struct RowResult {
 // grid: (tile of rows, chunk of keys, (sequence, head)) from one index.  part != nullptr: partial results, [chunk][slab][row][D]
 // normalized fp32 and the base-2 logarithm of their sums.
 template <int D, int NG, int QT>
-__global__ void __launch_bounds__(WAVES * 64, QT == 1 ? 3 : 2)
+__global__ void __launch_bounds__(WAVES * 64, QT == 1 && NG * D < 512 ? 3 : 2)
 cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides os, float* __restrict__ lse, float* __restrict__ part,
                    float* __restrict__ part_lse, int tiles, int n_splits, int chunk) {
     constexpr int CT = D / 16, STEPS = D / 32 / NG;
@@ -385,6 +386,7 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
     constexpr int MERGE = WAVES * CT * 64 * 16, STAGE = WAVES * (int)sizeof(Lds);
     __shared__ __attribute__((aligned(16))) unsigned char lds[MERGE > STAGE ? MERGE : STAGE];
     __shared__ float s_m[WAVES][16], s_l[WAVES][16];
+    const unsigned thousand = thousands();
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
     const RowsPlace at(c, q, tiles, n_splits);
     const int b = at.slab / c.heads, head = at.slab - b * c.heads, share = q.Hq / c.heads;
@@ -458,7 +460,7 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
                     c4f a[QT];
 #pragma unroll
                     for (int n = 0; n < STEPS; ++n) {
-                        const half8 k = operand(kw[g * STEPS + n]);
+                        const half8 k = operand(kw[g * STEPS + n], thousand);
 #pragma unroll
                         for (int i = 0; i < QT; ++i)
                             a[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, query[i].op[g * STEPS + n], n == 0 ? (c4f){0.0f, 0.0f, 0.0f, 0.0f} : a[i], 0, 0, 0);
@@ -506,7 +508,7 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
                 // V transposed: channel 16 ct + lane % 16, nibble i of the words: key 16 (i / 4) + 4 h + i % 4
                 const c2i vt = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
                     (__attribute__((address_space(3))) c2i*)(mine.v + v_chunk<D>(v_key, ct >> 1) + 8 * (ct & 1)));
-                const half8 v = operand((unsigned)vt[u]);
+                const half8 v = operand((unsigned)vt[u], thousand);
 #pragma unroll
                 for (int i = 0; i < QT; ++i) o[i][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[i][ct * NG / CT], o[i][ct], 0, 0, 0);
             }
@@ -610,6 +612,7 @@ cache4_attn_rows_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStr
     constexpr int QT = 2, CT = D / 16, STEPS = D / 32 / NG, RAW = TILE * D / 8;
     __shared__ TileStage<D, NG> stage[2];
     __shared__ __attribute__((aligned(16))) unsigned char raw_v[WAVES][RAW];
+    const unsigned thousand = thousands();
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
     const RowsPlace at(c, q, tiles, n_splits);
     const int b = at.slab / c.heads, head = at.slab - b * c.heads, share = q.Hq / c.heads;
@@ -654,15 +657,15 @@ cache4_attn_rows_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStr
             *(scale_t*)((wave == 0 ? to.ks : to.vs) + lane * NG) = absent ? (scale_t)(0) : own.scale;
         }
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) to.k[wave][i][lane] = operand(own.k[i]);
+        for (int i = 0; i < D / 32; ++i) to.k[wave][i][lane] = operand(own.k[i], thousand);
         wave_order();
         // V transposed: lane's channel, nibble i of the words: key 16 (i / 4) + 4 h + i % 4
         const int v_key = 16 * (col >> 2) + 4 * h + (col & 3);
 #pragma unroll
         for (int n = 0; n < D / 64; ++n) {
             const c2i x = __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) c2i*)(raw_v[wave] + v_key * (D / 8) + 8 * n));
-            to.v[0][D / 64 * wave + n][lane] = operand((unsigned)x[0]);
-            to.v[1][D / 64 * wave + n][lane] = operand((unsigned)x[1]);
+            to.v[0][D / 64 * wave + n][lane] = operand((unsigned)x[0], thousand);
+            to.v[1][D / 64 * wave + n][lane] = operand((unsigned)x[1], thousand);
         }
     };
     unsigned bad = 0;
@@ -962,6 +965,7 @@ __global__ void __launch_bounds__(WAVES * 64, 4) cache4_weights_few_kernel(Cache
     __shared__ __attribute__((aligned(16))) _Float16 s_ks[WAVES][TILE * NG];
     // (the sums wait here for one pass at the end: stores between the tiles would be waited for with the next tile's loads)
     __shared__ __attribute__((aligned(16))) float s_sum[FEW_CHUNK];
+    const unsigned thousand = thousands();
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
     const int slab = blockIdx.y, b = slab / c.heads, head = slab - b * c.heads, share = q.Hq / c.heads;
     const RowRange range(c, q, b, share);
@@ -1012,7 +1016,7 @@ __global__ void __launch_bounds__(WAVES * 64, 4) cache4_weights_few_kernel(Cache
                 LaneScales<NG> ks;
                 lane_scales<NG>(s_ks[wave], 16 * j + col, ks);
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) k[i] = operand(words[j][i]);
+                for (int i = 0; i < D / 32; ++i) k[i] = operand(words[j][i], thousand);
                 sum[j] = piece_weights<D, NG>(query.op, k, ks, rows, k0 + 16 * j + col, k0 + TILE <= first_end);
             }
             put_sums(sum, bad, s_sum + (k0 - k_begin), lane);
@@ -1031,6 +1035,7 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache4_weights_kernel(Cache4 c,
     __shared__ __attribute__((aligned(16))) float s_sum[WAVES * TILE];
     __shared__ __attribute__((aligned(16))) float s_sc[WAVES][16], s_reference[WAVES][16];
     __shared__ __attribute__((aligned(16))) int s_end[WAVES][16];
+    const unsigned thousand = thousands();
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
     const int slab = blockIdx.y, b = slab / c.heads, head = slab - b * c.heads, share = q.Hq / c.heads;
     const RowRange range(c, q, b, share);
@@ -1053,7 +1058,7 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache4_weights_kernel(Cache4 c,
             for (int j = 0; j < 4; ++j) {
                 lane_scales<NG>(s_ks[wave], 16 * j + col, ks[j]);
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) k[j][i] = operand(tile.k[j][i]);
+                for (int i = 0; i < D / 32; ++i) k[j][i] = operand(tile.k[j][i], thousand);
             }
         }
         // the first row that sees a key of the workgroup
@@ -1109,6 +1114,7 @@ __global__ void __launch_bounds__(NW * 64, 2) cache4_weights_rows_kernel(Cache4 
                                                                             const float* weights, float* out, int width) {
     __shared__ __attribute__((aligned(16))) _Float16 s_ks[NW][TILE * NG];
     __shared__ __attribute__((aligned(16))) float s_sum[NW][TILE];
+    const unsigned thousand = thousands();
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
     const int slab = blockIdx.y, b = slab / c.heads, head = slab - b * c.heads, share = q.Hq / c.heads;
     const RowRange range(c, q, b, share);
@@ -1133,7 +1139,7 @@ __global__ void __launch_bounds__(NW * 64, 2) cache4_weights_rows_kernel(Cache4 
             for (int j = 0; j < 4; ++j) {
                 lane_scales<NG>(s_ks[wave], 16 * j + col, ks[j]);
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) k[j][i] = operand(tile.k[j][i]);
+                for (int i = 0; i < D / 32; ++i) k[j][i] = operand(tile.k[j][i], thousand);
             }
         }
         SomeRows<D> some;

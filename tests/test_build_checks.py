@@ -229,3 +229,14 @@ def test_spills_among_the_products():
     assert len(problems) == 1 and "ILi128E" in problems[0]
     merge = "_ZN4sage19cache4_merge_kernelILi64E:\n\tscratch_load_dword v1, off, off\n.Lfunc_end2:\n"
     assert len(check_cache4_attn_asm(clean + merge)) == 1
+
+
+def test_inline_assembly_among_the_products():
+    """It is let pass before the first matrix instruction, and where it is empty (which only orders what the compiler does)."""
+    from paper_2410_02367_amd.build import check_cache4_attn_asm
+    line = "\t;;#ASMSTART\n%s\t;;#ASMEND"
+    kernel = "_ZN4sage18cache4_attn_kernelILi%dE:\n%s\n\tv_mfma_f32_16x16x32_f16 a\n%s\n\tv_mfma_f32_16x16x32_f16 b\n\ts_endpgm\n.Lfunc_end%d:\n"
+    clean = kernel % (64, line % "\tv_mov_b32 v0, 1\n", line % "", 0)
+    assert check_cache4_attn_asm(clean) == []
+    problems = check_cache4_attn_asm(clean + kernel % (128, "", line % "\tv_and_or_b32 v1, v2, s0, v3\n", 1))
+    assert len(problems) == 1 and "ILi128E" in problems[0] and "inline assembly" in problems[0]
