@@ -905,8 +905,8 @@ struct SomeRows {
     __device__ __forceinline__ float reference() const { return end > 0 ? row_reference(lse) : __builtin_inff(); }
 };
 template <int NG> using LaneScales = unsigned[(NG + 1) / 2];
-// -> the weights that 16 rows give to the lane's key, rows 4 h .. 4 h + 3 of them; key: the slot.  whole: every row sees it
-template <int D, int NG>
+// -> the weights that 16 rows give to the lane's key, the first R of the rows 4 h .. 4 h + 3; key: the slot.  whole: every row sees it
+template <int D, int NG, int R = 4>
 __device__ __forceinline__ float piece_weights(const half8 (&q)[D / 32], const half8 (&k)[D / 32], const LaneScales<NG>& ks, const LaneRows& rows, int key,
                                                bool whole) {
     constexpr int STEPS = D / 32 / NG;
@@ -917,11 +917,11 @@ __device__ __forceinline__ float piece_weights(const half8 (&q)[D / 32], const h
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) a = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[g * STEPS + i], k[g * STEPS + i], a, 0, 0, 0);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s[r] = __builtin_fmaf((float)half_of(ks[g / 2], g & 1), a[r], g == 0 ? 0.0f : s[r]);
+        for (int r = 0; r < R; ++r) s[r] = __builtin_fmaf((float)half_of(ks[g / 2], g & 1), a[r], g == 0 ? 0.0f : s[r]);
     }
     float sum = 0.0f;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < R; ++r) {
         const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], rows.sc[r], -rows.reference[r]));
         sum += whole || key < rows.end[r] ? p : 0.0f;
     }
@@ -958,8 +958,9 @@ __device__ __forceinline__ void add_sums(const float* sums, const float* had, fl
 }
 }  // namespace
 
-// At most 16 rows (a decoding step): their operands stay in registers, a wavefront walks tiles of keys, the next one on its way.
-template <int D, int NG>
+// At most 4 R rows (a decoding step): their operands stay in registers, a wavefront walks tiles of keys, the next one on its way.  Row i
+// is row 4 (i / R) + i % R of the product, so that a lane has R of them and none of its arithmetic is for rows that are not there.
+template <int D, int NG, int R>
 __global__ void __launch_bounds__(WAVES * 64, 4) cache4_weights_few_kernel(Cache4 c, CacheQueries q, const float* __restrict__ lse,
                                                                         const float* weights, float* out, int width, int chunk) {
     __shared__ __attribute__((aligned(16))) _Float16 s_ks[WAVES][TILE * NG];
@@ -982,16 +983,17 @@ __global__ void __launch_bounds__(WAVES * 64, 4) cache4_weights_few_kernel(Cache
         pages.look_up(c, table, k0);
         tile.request(c, head_at, pages, k0, lane);
         pages.look_up(c, table, k0 + NEXT);
-        const int row = min(col, range.rows - 1), tq = row / share, g = row - tq * share;
+        const int at = (col >> 2) * R + (col & 3), row = min(at, range.rows - 1), tq = row / share, g = row - tq * share;
+        const bool is = (col & 3) < R && at < range.rows;
         const int first_end = range.end(0, q.causal);
         Queries4<D> query;
         const float sc = query.load(q, b * q.strides.b + (head * share + g) * q.strides.h + tq * q.strides.n, h);
         // (of 16 rows those that are not there leave no weight either)
-        const float reference = col < range.rows ? row_reference(lse[((size_t)b * q.Hq + head * share + g) * q.Nq + tq]) : __builtin_inff();
-        const int end = col < range.rows ? range.end(tq, q.causal) : 0;
+        const float reference = is ? row_reference(lse[((size_t)b * q.Hq + head * share + g) * q.Nq + tq]) : __builtin_inff();
+        const int end = is ? range.end(tq, q.causal) : 0;
         LaneRows rows;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        for (int r = 0; r < R; ++r) {
             rows.sc[r] = __shfl(sc, 4 * h + r, 64);
             rows.reference[r] = __shfl(reference, 4 * h + r, 64);
             rows.end[r] = __shfl(end, 4 * h + r, 64);
@@ -1017,7 +1019,7 @@ __global__ void __launch_bounds__(WAVES * 64, 4) cache4_weights_few_kernel(Cache
                 lane_scales<NG>(s_ks[wave], 16 * j + col, ks);
 #pragma unroll
                 for (int i = 0; i < D / 32; ++i) k[i] = operand(words[j][i], thousand);
-                sum[j] = piece_weights<D, NG>(query.op, k, ks, rows, k0 + 16 * j + col, k0 + TILE <= first_end);
+                sum[j] = piece_weights<D, NG, R>(query.op, k, ks, rows, k0 + 16 * j + col, k0 + TILE <= first_end);
             }
             put_sums(sum, bad, s_sum + (k0 - k_begin), lane);
         }
@@ -1278,8 +1280,9 @@ constexpr int NARROW = 256;
 hipError_t launch_cache4_weights(const Cache4& c, const CacheQueries& q, const float* lse, const float* weights, float* out, int width,
                                  hipStream_t st) {
     const int slabs = q.B * c.heads, ng = c.groups, tiles = (width + WAVES * TILE - 1) / (WAVES * TILE);
-    const bool few = q.Hq / c.heads * q.Nq <= 16;
-    const bool narrow = (long)tiles * slabs < NARROW && q.Hq / c.heads * q.Nq > 64, eight = (long)tiles * slabs <= NARROW / 4;
+    const int rows = q.Hq / c.heads * q.Nq;
+    const bool few = rows <= 16;
+    const bool narrow = (long)tiles * slabs < NARROW && rows > 64, eight = (long)tiles * slabs <= NARROW / 4;
     // few rows: as many workgroups as the attention has, so that a wavefront has tiles to walk
     int chunks = few ? WANTED_FEW / slabs : tiles;
     if (chunks < 1) chunks = 1;
@@ -1288,7 +1291,9 @@ hipError_t launch_cache4_weights(const Cache4& c, const CacheQueries& q, const f
     const dim3 grid((width + chunk - 1) / chunk, slabs), by_64((width + TILE - 1) / TILE, slabs);
 #define SAGE_CACHE4_WEIGHTS(D, NG)                                                                                          \
     do {                                                                                                                     \
-        if (few) cache4_weights_few_kernel<D, NG><<<grid, WAVES * 64, 0, st>>>(c, q, lse, weights, out, width, chunk);        \
+        if (rows <= 4) cache4_weights_few_kernel<D, NG, 1><<<grid, WAVES * 64, 0, st>>>(c, q, lse, weights, out, width, chunk);      \
+        else if (rows <= 8) cache4_weights_few_kernel<D, NG, 2><<<grid, WAVES * 64, 0, st>>>(c, q, lse, weights, out, width, chunk); \
+        else if (few) cache4_weights_few_kernel<D, NG, 4><<<grid, WAVES * 64, 0, st>>>(c, q, lse, weights, out, width, chunk);       \
         else if (narrow && eight) cache4_weights_rows_kernel<D, NG, 8><<<by_64, 8 * 64, 0, st>>>(c, q, lse, weights, out, width); \
         else if (narrow) cache4_weights_rows_kernel<D, NG, 4><<<by_64, 4 * 64, 0, st>>>(c, q, lse, weights, out, width);      \
         else cache4_weights_kernel<D, NG><<<grid, WAVES * 64, 0, st>>>(c, q, lse, weights, out, width);                       \

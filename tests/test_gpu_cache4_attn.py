@@ -66,6 +66,13 @@ def test_heads_and_queries(Hq, Hkv, Nq, D, group, page):
     case(Hq + Nq, 2, Hq, Hkv, Nq, D, page, group, "f16", [Nq + 83, max(1, Nq - 1)])
 
 
+# 3 to 16 rows of queries per key head: one, two and four of them per lane
+@pytest.mark.parametrize("D,group,page", FORMS)
+@pytest.mark.parametrize("Hq,Hkv,Nq", [(3, 1, 1), (5, 1, 1), (14, 2, 1), (8, 1, 1), (9, 1, 1), (6, 2, 5), (16, 1, 1)])
+def test_a_few_rows(Hq, Hkv, Nq, D, group, page):
+    case(100 + Hq + Nq, 3, Hq, Hkv, Nq, D, page, group, "bf16", [Nq + 83, 2, 300], count=[Nq, 1, max(1, Nq - 1)])
+
+
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("D,group,page", FORMS[1:4])
 def test_padded_batch(D, group, page, causal):
