@@ -549,6 +549,224 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
     }
 }
 
+// ---- at most four rows (a decoding step of up to four query heads per key head)
+namespace {
+// the sum over the lanes 4 apart of 16, in all of them
+__device__ __forceinline__ float over_fours(float x) {
+    const auto turned = [](float v, auto ctrl) {
+        const int i = __builtin_bit_cast(int, v);
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, decltype(ctrl)::value, 0xF, 0xF, false));
+    };
+    x += turned(x, std::integral_constant<int, 0x128>{});        // the lane 8 before, round 16
+    return x + turned(x, std::integral_constant<int, 0x124>{});  // 4 before
+}
+}  // namespace
+
+// With four rows a quarter of the score products' columns would be of use.  Column 4 j + c of them is row c for the keys of piece j: the
+// queries of piece j's product are zero in the other columns, and the four products of a tile add up into one.  A lane has 4
+// scores per tile instead of 16 and weighs those; its weights stand, in its column of the second product, at the keys of its
+// piece beside zeros, and the columns of a row are added up at the end.
+template <int D, int NG>
+__global__ void __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2)
+cache4_attn_few_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides os, float* __restrict__ lse, float* __restrict__ part,
+                       float* __restrict__ part_lse, int n_splits, int chunk) {
+    constexpr int CT = D / 16, STEPS = D / 32 / NG;
+    typedef WaveLds<D, NG> Lds;
+    constexpr int MERGE = WAVES * CT * 16 * 16, STAGE = WAVES * (int)sizeof(Lds);
+    __shared__ __attribute__((aligned(16))) unsigned char lds[MERGE > STAGE ? MERGE : STAGE];
+    __shared__ float s_m[WAVES][4], s_l[WAVES][4];
+    const unsigned thousand = thousands();
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
+    const int own = col & 3, piece = col >> 2;                      // the column's row, and the keys it has
+    const RowsPlace at(c, q, 1, n_splits);
+    const int b = at.slab / c.heads, head = at.slab - b * c.heads, share = q.Hq / c.heads;
+    const RowRange range(c, q, b, share);
+    const int all_rows = q.Nq * share;
+    const int first_end = range.rows > 0 ? range.end(0, q.causal) : 0, last_end = range.rows > 0 ? range.end(range.count - 1, q.causal) : 0;
+    const int k_begin = at.split * chunk, k_end = min(k_begin + chunk, last_end);
+    if (part != nullptr && k_begin >= last_end) return;              // (the merge knows)
+
+    half8 query[4][D / 32];
+    float sc, M = UNSET, l = 0.0f;
+    int end;
+    {
+        const int row = min(own, max(range.rows - 1, 0)), tq = row / share, g = row - tq * share;
+        Queries4<D> mine;
+        sc = mine.load(q, b * q.strides.b + (head * share + g) * q.strides.h + tq * q.strides.n, h);
+        end = range.end(tq, q.causal);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) query[j][i] = piece == j ? mine.op[i] : (half8){};
+    }
+    // what brings half r % 2 of a register to where the weights of keys r of the pieces 2 u (low) and 2 u + 1 (high) stand
+    unsigned place[2][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const unsigned bytes = r ? 0x0302u : 0x0100u;
+            place[u][r] = piece == 2 * u ? 0x0c0c0000u | bytes : piece == 2 * u + 1 ? bytes << 16 | 0x0c0cu : 0x0c0c0c0cu;
+        }
+    c4f o[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) o[ct] = (c4f){0.0f, 0.0f, 0.0f, 0.0f};
+
+    Lds& mine = *(Lds*)(lds + wave * sizeof(Lds));
+    const int* const table = c.table + (size_t)b * c.columns;
+    const unsigned char* const head_at = c.data + (size_t)head * c.block_bytes;
+    typedef KeyTile<D, NG, true> Tile;
+    typedef typename Tile::words words;
+    typedef unsigned scales_t __attribute__((ext_vector_type(2 * NG)));
+    constexpr int NEXT = TILE * WAVES;
+    Tile tile;
+    PageIds pages;
+    int k0 = k_begin + TILE * wave;
+    if (k0 < k_end) {
+        pages.look_up(c, table, k0);
+        tile.request(c, head_at, pages, k0, lane);
+        pages.look_up(c, table, k0 + NEXT);
+    }
+    for (; k0 < k_end; k0 += NEXT) {
+        wave_order();
+        // ---- the tile to LDS.  The scales of a row past the last key are perhaps no numbers: 0 instead.
+        const unsigned bad = tile.bad;
+        const bool absent = k0 + lane >= last_end || (bad >> h & 1);
+        *(typename Tile::scale_t*)(mine.ks + lane * NG) = absent ? (typename Tile::scale_t)(0) : tile.ks;
+        *(typename Tile::scale_t*)(mine.vs + lane * NG) = absent ? (typename Tile::scale_t)(0) : tile.vs;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) *(c4u*)(mine.v + v_chunk<D>((i * 1024 + lane * 16) / (D / 2), lane % (D / 32))) = tile.v[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ((words*)mine.k)[j * 64 + lane] = tile.k[j];
+        wave_order();
+        if (k0 + NEXT < k_end) {
+            tile.request(c, head_at, pages, k0 + NEXT, lane);
+            pages.look_up(c, table, k0 + 2 * NEXT);
+        }
+        // ---- scores of keys 16 piece + 4 h + r for row `own`
+        const int key = 16 * piece + 4 * h;
+        const scales_t ks = *(const scales_t*)(mine.ks + key * NG), vs = *(const scales_t*)(mine.vs + key * NG);
+        c4f a[NG];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const words kw = ((const words*)mine.k)[j * 64 + lane];
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int n = 0; n < STEPS; ++n)
+                    a[g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(kw[g * STEPS + n], thousand), query[j][g * STEPS + n],
+                                                                  j == 0 && n == 0 ? (c4f){0.0f, 0.0f, 0.0f, 0.0f} : a[g], 0, 0, 0);
+        }
+        float s[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int g = 0; g < NG; ++g) s[r] = __builtin_fmaf((float)half_of(ks[(r * NG + g) / 2], (r * NG + g) & 1), a[g][r], g == 0 ? 0.0f : s[r]);
+        if (k0 + TILE > first_end || bad != 0) {
+            const int last = bad >> piece & 1 ? 0 : end;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (k0 + key + r >= last) s[r] = -__builtin_inff();
+        }
+        // ---- weights, as weigh() forms them: two keys to a register
+        unsigned x[NG][2];
+        float sum;
+        auto weights = [&] {
+            typedef float f2 __attribute__((ext_vector_type(2)));
+            typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+            float p[4];
+            sum = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, r & 1 ? -(M + 4.0f) : -M));
+                sum = r & 1 ? __builtin_fmaf(p[r], 16.0f, sum) : sum + p[r];
+            }
+            unsigned top = 0;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+#pragma unroll
+                for (int r = 0; r < 4; r += 2) {
+                    const f2 y = {__builtin_fmaf(p[r], (float)half_of(vs[(r * NG + g) / 2], (r * NG + g) & 1), 0.0f),
+                                  __builtin_fmaf(p[r + 1], (float)half_of(vs[((r + 1) * NG + g) / 2], ((r + 1) * NG + g) & 1), 0.0f)};
+                    x[g][r / 2] = __builtin_bit_cast(unsigned, __builtin_convertvector(y, h2));
+                }
+                top = max3_pairs(top, x[g][0], x[g][1]);
+            }
+            return __builtin_amdgcn_ballot_w64(sum > P_LIMIT || half_of(top, 0) > W_LIMIT || half_of(top, 1) > W_LIMIT) != 0ull;
+        };
+        if (__builtin_expect(weights(), 0)) {
+            float most = -__builtin_inff();
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float scale = SMALLEST;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) scale = __builtin_fmaxf(scale, (float)half_of(vs[(r * NG + g) / 2], (r * NG + g) & 1));
+                most = __builtin_fmaxf(most, __builtin_fmaf(s[r], sc, __builtin_amdgcn_logf(scale) - RAISE));
+            }
+            most = __builtin_fmaxf(most, __shfl_xor(most, 4, 64));
+            most = __builtin_fmaxf(most, __shfl_xor(most, 8, 64));
+            const float M_new = __builtin_fmaxf(M, over_h(most, false)), alpha = __builtin_amdgcn_exp2f(M - M_new);
+            M = M_new;
+            l *= alpha;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) o[ct] *= alpha;
+            weights();
+        }
+        l += sum;
+        half8 w[2][NG];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+                w[u][g] = __builtin_bit_cast(half8, (c4u){__builtin_amdgcn_perm(0u, x[g][0], place[u][0]), __builtin_amdgcn_perm(0u, x[g][0], place[u][1]),
+                                                         __builtin_amdgcn_perm(0u, x[g][1], place[u][0]), __builtin_amdgcn_perm(0u, x[g][1], place[u][1])});
+        const int v_key = 16 * (col >> 2) + 4 * h + (col & 3);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            // V transposed: channel 16 ct + lane % 16, nibble i of the words: key 16 (i / 4) + 4 h + i % 4
+            const c2i vt = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
+                (__attribute__((address_space(3))) c2i*)(mine.v + v_chunk<D>(v_key, ct >> 1) + 8 * (ct & 1)));
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand((unsigned)vt[u], thousand), w[u][ct * NG / CT], o[ct], 0, 0, 0);
+        }
+    }
+
+    // ---- the columns' and the wavefronts' results: O = sum f_w O_w / sum f_w l_w, f_w = 2^(M_w - max M)
+    const float lw = over_fours(over_h(l, true));
+    __syncthreads();                    // the tiles have been read
+    if (lane < 4) {
+        s_m[wave][own] = M;
+        s_l[wave][own] = lw;
+    }
+    __syncthreads();
+    float top = s_m[0][own], total = 0.0f;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) top = __builtin_fmaxf(top, s_m[w][own]);
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) total = __builtin_fmaf(s_l[w][own], __builtin_amdgcn_exp2f(s_m[w][own] - top), total);
+    const float f = __builtin_amdgcn_exp2f(M - top);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        c4f x;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = over_fours(o[ct][r]) * f;
+        if (piece == 0) *(c4f*)(lds + ((wave * CT + ct) * 16 + 4 * h + own) * 16) = x;
+    }
+    __syncthreads();
+    if (piece != 0 || own >= all_rows) return;
+    const RowResult r(at, q, head, share, own, own < range.rows, top, total, all_rows);
+    if (wave == 0 && h == 0) r.put_sum(q, lse, part_lse, part != nullptr);
+#pragma unroll
+    for (int n = 0; n < CT / WAVES; ++n) {
+        const int ct = wave + WAVES * n;
+        c4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) x += *(const c4f*)(lds + ((w * CT + ct) * 16 + 4 * h + own) * 16);
+        r.template put<D>(q, out, os, part, x, 16 * ct + 4 * h);
+    }
+}
+
 // ---- many rows: operands made once for all of a workgroup's wavefronts
 namespace {
 // A wavefront's share of a tile of 64 keys, as it comes from memory: K's words of piece `wave`, a quarter of every V row, the
@@ -1242,7 +1460,8 @@ static void launch_attn_form(const AttnPlan& p, const Cache4& c, const CacheQuer
                              float* part_lse, hipStream_t st) {
     const unsigned grid = (unsigned)(q.B * c.heads * p.tiles * p.n_splits);
 #define SAGE_CACHE4_ATTN(QT) cache4_attn_kernel<D, NG, QT><<<grid, WAVES * 64, 0, st>>>(c, q, out, os, lse, part, part_lse, p.tiles, p.n_splits, p.chunk)
-    if (p.rows == 16) SAGE_CACHE4_ATTN(1);
+    if (q.Hq / c.heads * q.Nq <= 4) cache4_attn_few_kernel<D, NG><<<grid, WAVES * 64, 0, st>>>(c, q, out, os, lse, part, part_lse, p.n_splits, p.chunk);
+    else if (p.rows == 16) SAGE_CACHE4_ATTN(1);
     else if (p.rows == 32) SAGE_CACHE4_ATTN(2);
     else cache4_attn_rows_kernel<D, NG><<<grid, WAVES * 64, 0, st>>>(c, q, out, os, lse, part, part_lse, p.tiles, p.n_splits, p.chunk);
 #undef SAGE_CACHE4_ATTN
