@@ -377,6 +377,7 @@ struct RowResult {
 
 // grid: (tile of rows, chunk of keys, (sequence, head)) from one index.  part != nullptr: partial results, [chunk][slab][row][D]
 // normalized fp32 and the base-2 logarithm of their sums.
+// (Three wavefronts per SIMD where 168 registers are enough: with four scales of 128 channels they are not, 119 us for 117.)
 template <int D, int NG, int QT>
 __global__ void __launch_bounds__(WAVES * 64, QT == 1 && NG * D < 512 ? 3 : 2)
 cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides os, float* __restrict__ lse, float* __restrict__ part,
@@ -565,7 +566,9 @@ __device__ __forceinline__ float over_fours(float x) {
 // With four rows a quarter of the score products' columns would be of use.  Column 4 j + c of them is row c for the keys of piece j: the
 // queries of piece j's product are zero in the other columns, and the four products of a tile add up into one.  A lane has 4
 // scores per tile instead of 16 and weighs those; its weights stand, in its column of the second product, at the keys of its
-// piece beside zeros, and the columns of a row are added up at the end.
+// piece beside zeros, and the columns of a row are added up at the end.  489 vector instructions per tile for 644; 256 slabs of 8K to 16K keys
+// of 128 channels 104 us for 119, the same loads alone 82.  (The queries in LDS, for three wavefronts per
+// SIMD instead of two: 104.)
 template <int D, int NG>
 __global__ void __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2)
 cache4_attn_few_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides os, float* __restrict__ lse, float* __restrict__ part,
