@@ -217,3 +217,26 @@ def test_strides():
     sage.sage_cache4_attn(q, *args, page=page, out=frame[:, :, 1:].transpose(1, 2))
     assert torch.equal(frame[:, :, 1:].transpose(1, 2), want) and torch.all(frame[:, :, 0] == 7.0)
     assert torch.equal(sage.sage_cache4_weights(q, *args, lse, page=page), sage.sage_cache4_weights(q.contiguous(), *args, lse, page=page))
+
+
+# at most four rows: their kernel's raised references, absent pages, cut keys, and rows that are no numbers
+@pytest.mark.parametrize("D,group,page", FORMS)
+@pytest.mark.parametrize("Hq,Hkv,Nq", [(1, 1, 1), (4, 2, 2), (3, 1, 1), (4, 1, 1), (2, 1, 2), (1, 1, 4)])
+def test_up_to_four_rows(Hq, Hkv, Nq, D, group, page):
+    case(50 + Hq + Nq, 2, Hq, Hkv, Nq, D, page, group, "f16", [1300, 333], q_gain=25.0, bad=[(0, 1), (1, 0)])
+    case(60 + Hq + Nq, 3, Hq, Hkv, Nq, D, page, group, "bf16", [700, 3, 64], count=[Nq, 1, 0], n_splits=3, q_gain=10.0, causal=False)
+
+
+@pytest.mark.parametrize("D,group,page", FORMS)
+def test_four_rows_of_which_one_is_no_number(D, group, page):
+    import paper_2410_02367_amd as sage
+    n = 300
+    c, table = make_cache(71, 1, 1, D, page, group, [n], -(-n // page))
+    q = rounded(np.random.default_rng(71).standard_normal((1, 4, 1, D)) * 3, "f16")
+    args = (dev(c.data), dev(table), dev(np.int32([n])))
+    clean, lse = sage.sage_cache4_attn(dev(q, torch.float16), *args, page=page, group=group, return_lse=True)
+    q[0, 2, 0, 5] = np.nan
+    out, got = sage.sage_cache4_attn(dev(q, torch.float16), *args, page=page, group=group, return_lse=True)
+    rest = [0, 1, 3]
+    assert torch.equal(out[0, rest], clean[0, rest]) and torch.equal(got[0, rest], lse[0, rest])
+    assert torch.isnan(out[0, 2]).all() and torch.isnan(got[0, 2]).all()
