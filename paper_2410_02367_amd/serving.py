@@ -127,7 +127,8 @@ def sage_rope_frequencies(rotated: int, base: float = 10000.0, scaling: str | No
         else:
             def pair(turns):            # index of the pair that turns so often
                 return rotated * math.log(original_length / (turns * 2 * math.pi)) / (2 * math.log(base))
-            first, last = max(math.floor(pair(high)), 0), min(math.ceil(pair(low)), rotated // 2 - 1)
+            # (where all pairs turn more than `low` times the ramp ends behind the last one)
+            first, last = max(math.floor(pair(high)), 0), min(math.ceil(pair(low)), rotated - 1)
             stay = 1.0 - ((index / 2 - first) / max(last - first, 1e-3)).clamp(0.0, 1.0)
             amplitude = 0.1 * math.log(factor) + 1.0
         freq = freq * stay + freq / factor * (1.0 - stay)
