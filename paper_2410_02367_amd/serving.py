@@ -97,7 +97,7 @@ def _check(status, where):
 # ---- rotary positions
 
 def sage_rope_frequencies(rotated: int, base: float = 10000.0, scaling: str | None = None, factor: float = 1.0,
-                          original_length: int = 8192, low: float = 1.0, high: float = 4.0, device=None):
+                          original_length: int = 8192, low: float = 1.0, high: float | None = None, device=None):
     """Radians per position of each pair of channels, fp64 [rotated / 2], and the amplitude that goes with them.
     base^(-2 i / rotated), for contexts `factor` times as long as the model's own changed by `scaling`:
       None      not
@@ -106,7 +106,10 @@ def sage_rope_frequencies(rotated: int, base: float = 10000.0, scaling: str | No
       "parts"   a pair that turns less than `low` times in original_length positions divided by factor, more than `high` times
                 left, in between a mixture, linear in the number of turns
       "ramp"    the same with the mixture linear in the pair's index, and an amplitude of 0.1 ln(factor) + 1 (YaRN)
+    high None: 32 for "ramp", 4 otherwise.
     """
+    if high is None:
+        high = 32.0 if scaling == "ramp" else 4.0
     if rotated < 2 or rotated % 2 != 0:
         raise ValueError("rotated: an even number of channels")
     if not (base > 0 and factor >= 1 and original_length > 0 and 0 < low < high):

@@ -36,3 +36,16 @@ def test_a_slowest_pair_that_turns_is_not_divided_as_one_that_does_not(rotated, 
     assert original_length * slowest / (2 * math.pi) > 1.0                       # more than `low` times
     f, _ = sage.sage_rope_frequencies(rotated, scaling="ramp", factor=4.0, original_length=original_length, low=1.0, high=32.0)
     assert f[-1] > slowest / 4.0 * 1.25
+
+
+def test_the_turns_that_each_scaling_leaves_alone_by_default():
+    """"parts" mixes between 1 and 4 turns, "ramp" (YaRN) between 1 and 32."""
+    import paper_2410_02367_amd as sage
+    for scaling, high in (("parts", 4.0), ("ramp", 32.0)):
+        f, _ = sage.sage_rope_frequencies(128, scaling=scaling, factor=8.0)
+        g, _ = sage.sage_rope_frequencies(128, scaling=scaling, factor=8.0, low=1.0, high=high)
+        assert np.array_equal(f.numpy(), g.numpy())
+    np.testing.assert_allclose(sage.sage_rope_frequencies(128, scaling="ramp", factor=8.0)[0].numpy(), ramp(128, 1e4, 8.0, 8192, 1.0, 32.0), rtol=2.0 ** -48)
+    for bad in (dict(scaling="ramp", low=40.0), dict(scaling="parts", low=5.0), dict(low=2.0, high=1.0)):
+        with pytest.raises(ValueError):
+            sage.sage_rope_frequencies(64, **bad)
