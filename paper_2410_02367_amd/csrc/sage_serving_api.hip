@@ -182,7 +182,8 @@ int sage_cache4_evict(const void* cache, int num_pages, const int32_t* pages, in
     if (keep <= 0 || keep > out_columns * page || width < columns * page || width > (1 << 23) || out_width < keep || out_width > (1 << 23))
         return SAGE_ERR_SHAPE;
     // in place, or the old accumulators under the new ones: rows would be overwritten before they are read
-    if (recent < 0 || recent > keep || pages == out_pages || weights == out_weights || lengths == out_lengths) return SAGE_ERR_VALUE;
+    const bool in_place = cache == out_cache && pages == out_pages;
+    if (recent < 0 || recent > keep || in_place || weights == out_weights || lengths == out_lengths) return SAGE_ERR_VALUE;
     if (!aligned(lengths, 4) || !aligned(weights, 4) || !aligned(out_weights, 4) || !aligned(kept, 4) || !aligned(out_lengths, 4)) return SAGE_ERR_ALIGN;
     return status(sage::launch_cache4_evict(view(cache, pages, Hkv, D, num_pages, columns, page, group), lengths, weights, width,
                                             view(out_cache, out_pages, Hkv, D, out_num_pages, out_columns, page, group), out_weights, out_width,
