@@ -1,6 +1,7 @@
 """Binding of the serving calls of libsage.so (declared in include/sage.h): rotary positions, and the cache of K and V held
-in 4 bits with what works on it.  Argument marshalling only, as in :mod:`binding`, but for sage_rope_frequencies(): the extension
-module makes the calls that are in order, the code here the others, or their errors.
+in 4 bits with what works on it.  Argument marshalling only, as in :mod:`binding`, but for sage_rope_frequencies() and the gradients of
+the rotation: the extension module makes the calls that are in order, the code here the others, or their errors.  Results of the
+other calls take no part in autograd.
 
 Tensors are [B, H, N, D] with neighbouring channels and any distances between the rows (a transposed view of [B, N, H, D] as a
 projection leaves it is taken as it is); all of a call's tensors are on one device, which need not be the current one."""
@@ -166,9 +167,61 @@ def _rope(entry, x, y, positions, inv_freq, interleaved, amplitude, x_out, y_out
     return x_out if y is None else (x_out, y_out)
 
 
+def _tracked(*tensors) -> bool:
+    return any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors) and torch.is_grad_enabled()
+
+
+def _whole_rows(t):
+    """t, or a copy of it where its rows are not as the calls take them (a gradient may be an expanded number)."""
+    if t is None or t.shape[3] < 2 or (t.stride(3) == 1 and all(x % 16 == 0 for x in (t.data_ptr(), *(s * t.element_size() for s in t.stride()[:3])))):
+        return t
+    return t.clone(memory_format=torch.contiguous_format)
+
+
+class _Turn(torch.autograd.Function):
+    """The rotation, or where `back` the turn back, each the gradient of the other."""
+
+    @staticmethod
+    def forward(ctx, q, k, positions, inv_freq, interleaved, amplitude, back):
+        ctx.save_for_backward(positions, inv_freq)
+        ctx.form, ctx.back = (interleaved, amplitude), back
+        ctx.set_materialize_grads(False)
+        r = (sage_rope_bwd if back else sage_rope)(q, k, positions, inv_freq, interleaved, amplitude)
+        constant = [y for y, needed in zip((r,) if k is None else r, ctx.needs_input_grad) if not needed]
+        ctx.mark_non_differentiable(*constant)
+        return r
+
+    @staticmethod
+    def backward(ctx, *grads):
+        positions, inv_freq = ctx.saved_tensors
+        turn = sage_rope if ctx.back else sage_rope_bwd
+        grads = [_whole_rows(g if needed else None) for g, needed in zip((*grads, None), ctx.needs_input_grad)][:2]
+        there = [g for g in grads if g is not None]
+        if len(there) == 2:
+            grads = turn(*there, positions, inv_freq, *ctx.form)
+        elif there:
+            there = turn(there[0], None, positions, inv_freq, *ctx.form)
+            grads = [None if g is None else there for g in grads]
+        return (*grads, *[None] * 5)
+
+
+def _turn(back, q, k, positions, inv_freq, interleaved, amplitude, q_out, k_out, stream):
+    """A call that autograd takes note of."""
+    _tensor(q, "q", tuple(_TYPES), 4)
+    if q_out is not None or k_out is not None:
+        raise ValueError("q_out, k_out: an output of the caller's has no gradient, but an input requires one")
+    if _tracked(inv_freq):
+        raise ValueError("inv_freq: there is no gradient of the frequencies")
+    args = q, k, positions, inv_freq, interleaved, amplitude, back
+    return _there(q.device, stream, _Turn.apply, *args) if _elsewhere(q.device, stream) else _Turn.apply(*args)
+
+
 def sage_rope(q, k, positions, inv_freq, interleaved: bool = False, amplitude: float = 1.0, q_out=None, k_out=None, stream=None):
     """q [B,Hq,N,D] and k [B,Hk,N,D] (or None) with their pairs of channels turned by position * inv_freq -> (q', k'), or q'.
-    positions int32 [N] or [B,N]; inv_freq fp64 [rotated / 2], the channels from `rotated` on pass; outputs may be the inputs."""
+    positions int32 [N] or [B,N]; inv_freq fp64 [rotated / 2], the channels from `rotated` on pass; outputs may be the inputs.
+    Differentiable in q and k, where no output is given: the gradients are sage_rope_bwd()'s."""
+    if _tracked(q, k, inv_freq):
+        return _turn(False, q, k, positions, inv_freq, interleaved, amplitude, q_out, k_out, stream)
     r = _fast().rope(q, k, positions, inv_freq, interleaved, amplitude, q_out, k_out, _handle(stream))
     if r is not None:
         return _answer(r, "sage_rope")
@@ -176,7 +229,10 @@ def sage_rope(q, k, positions, inv_freq, interleaved: bool = False, amplitude: f
 
 
 def sage_rope_bwd(dq, dk, positions, inv_freq, interleaved: bool = False, amplitude: float = 1.0, dq_out=None, dk_out=None, stream=None):
-    """The gradients of sage_rope()'s inputs from those of its outputs, dq [B,Hq,N,D] and dk [B,Hk,N,D] (or None)."""
+    """The gradients of sage_rope()'s inputs from those of its outputs, dq [B,Hq,N,D] and dk [B,Hk,N,D] (or None).  Differentiable as
+    that is."""
+    if _tracked(dq, dk, inv_freq):
+        return _turn(True, dq, dk, positions, inv_freq, interleaved, amplitude, dq_out, dk_out, stream)
     r = _fast().rope_bwd(dq, dk, positions, inv_freq, interleaved, amplitude, dq_out, dk_out, _handle(stream))
     if r is not None:
         return _answer(r, "sage_rope_bwd")
