@@ -16,9 +16,17 @@
 //         fp16(exp2(s - M) * scale).  V is transposed by the LDS read that transposes nibbles; the keys of an operand are in
 //         the order in which the score tiles leave them, so P never leaves its registers.
 //
-// The reference M bounds what is rounded to fp16: it is raised where some exp2(s - M) * scale passes 2^12 (or the weights
-// of 32 keys 2^45), to the largest s + log2(scale) less 4.  So the fp16 range is spent on what reaches the output, whatever the scales
-// are: a key with large values and next to no weight leaves the others their precision.  The sums l and O are fp32.
+// What is rounded to fp16, a weight times its key's scale, is bounded by a reference R per row and group of channels: it is
+// exp2(s - R) * scale, and where one passes 2^15 (or the weights of 8 keys 2^50) R is raised to the largest s + log2(scale) less 10, rounded up
+// to a whole number.  So the range of fp16 is spent on what reaches the group's output, whatever the scales are: neither a key with large
+// values and next to no weight nor a group of larger values leaves others less precision.  M is the largest R of a row.  Groups that ask for
+// up to 7 less, or have had no value but 0, share it (their largest is 2^2 at least, so that what rounds to a subnormal number is off by 2^-23 of it), and as long
+// as all rows of a wavefront have nothing but M, which is the rule, a weight is one product.  Where they have not, 32 keys are weighed again with a
+// product more per group, and R follows the largest: 108 -> 127 us for 256 slabs of 8K to 16K keys with four rows and one group of four
+// 2^8 times the others, 116 -> 192 with 16 rows, 915 -> 2580 for 1024 queries of 32 heads on 32K keys.  (A product with a power of two
+// per row and group in any case: 719 us for 717 for those 1024 with two groups, 979 for 915 with four, 119 for 116 with the 16 rows.)
+// The weights in fp16 are a choice: with half a step of 2^-11 each they take the error of an fp16 output against 64 bits from 2.1e-4, its own
+// rounding, to 2.9e-4.  The sums l (with M) and O (each group with its R) are fp32.
 #include "sage_serving.h"
 #include "sage_device.h"
 
@@ -32,9 +40,9 @@ typedef int c2i __attribute__((ext_vector_type(2)));
 namespace {
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float UNSET = -1e30f;             // a reference below every score: the first key that is seen raises it
-constexpr _Float16 W_LIMIT = 4096.0f;
-constexpr float P_LIMIT = 0x1p45f;
-constexpr float RAISE = 4.0f, SMALLEST = 0x1p-36f;
+constexpr _Float16 W_LIMIT = 32768.0f;
+constexpr float P_LIMIT = 0x1p50f;
+constexpr float RAISE = 10.0f, ALIKE = 7.0f, FARTHEST = 100.0f, SMALLEST = 0x1p-36f;
 constexpr int TILE = 64, WAVES = 4, FEW_CHUNK = 2048;
 
 // 8 codes of a word -> operand registers: element 2 m + s is the code of nibble m + 4 s, times 16 where m is odd.  A nibble in the
@@ -234,12 +242,80 @@ __device__ __forceinline__ unsigned max3_pairs(unsigned a, unsigned b, unsigned 
 }
 __device__ __forceinline__ _Float16 half_of(unsigned w, int hi) { return __builtin_bit_cast(_Float16, (unsigned short)(hi ? w >> 16 : w)); }
 
+// x, and the compiler does not know that: what is seldom needed is not made ahead and kept in registers
+template <class T>
+__device__ __forceinline__ T anew(T x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// Groups of a wavefront's keys, a bit each: those that had no value but 0 so far, and of those the ones that have one in the present tile.
+// (An empty group asks for no reference: channels that only fill up a head would have one of their own for nothing.)
+template <int NG>
+struct EmptyGroups {
+    unsigned empty = (1u << NG) - 1u, fresh = 0;
+    // scales: those of the lane's key of a tile -> whether a group of them is no longer empty (the same in all lanes)
+    template <class S>
+    __device__ __forceinline__ bool look(S scales) {
+        unsigned seen = 0;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            unsigned short own;
+            if constexpr (NG == 4) own = (unsigned short)(scales[g / 2] >> 16 * (g & 1));
+            else own = (unsigned short)(scales >> 16 * g);
+            if (__builtin_amdgcn_ballot_w64((own & 0x7fff) != 0) != 0ull) seen |= 1u << g;
+        }
+        fresh = empty & seen;
+        empty &= ~seen;
+        return fresh != 0;
+    }
+};
+// The references of a row: M, and how far below it those of the groups are, whole numbers in 8 bits each.
+template <int NG>
+struct References {
+    float M;
+    unsigned below;
+    __device__ __forceinline__ void clear() {
+        M = UNSET;
+        below = 0;
+    }
+    __device__ __forceinline__ int distance(int g) const { return NG == 1 ? 0 : (int)(below >> 8 * g & 255u); }
+    // what brings sums of group g to M
+    __device__ __forceinline__ float back(int g) const { return ldexpf(1.0f, -distance(g)); }
+    // raised to what the row's keys ask for; alpha: what the groups' sums so far are multiplied by -> what l is (whole powers of two)
+    __device__ __forceinline__ float raise(const float (&most)[NG], const EmptyGroups<NG>& groups, float (&alpha)[NG]) {
+        const float M_old = M;
+        float R[NG];
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            R[g] = __builtin_fmaxf(groups.fresh >> g & 1 ? UNSET : M_old - (float)distance(g), __builtin_ceilf(most[g]));
+            M = __builtin_fmaxf(M, R[g]);
+        }
+        unsigned now = 0;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            const float d = M - R[g] <= ALIKE || (groups.empty >> g & 1) || R[g] == UNSET ? 0.0f : __builtin_fminf(M - R[g], FARTHEST);
+            alpha[g] = __builtin_amdgcn_exp2f((M_old - M) + (d - (float)distance(g)));
+            now |= (unsigned)d << 8 * g;
+        }
+        below = now;
+        return __builtin_amdgcn_exp2f(M_old - M);
+    }
+    // whether the rows of the wavefront have nothing but M (the same in all lanes)
+    __device__ __forceinline__ bool alike() const { return NG == 1 || __builtin_amdgcn_ballot_w64(below != 0u) == 0ull; }
+};
+
 // The weights of 32 keys for 16 rows: register r of the two score tiles is keys 4 h + r and 16 + 4 h + r, element 2 r and 2 r + 1
-// of an operand; those of odd r meet 16-fold codes and are 2^-4 of the others.  -> whether the reference is too low.
-template <int NG, class S>
-__device__ __forceinline__ bool weigh(const float (&s)[2][4], float sc, float M, const S (&vs)[2], half8 (&w)[NG], float& sum) {
+// of an operand; those of odd r meet 16-fold codes and are 2^-4 of the others.  PLAIN: with M for all groups.  -> whether a reference is too low.
+template <bool PLAIN, int NG, class S>
+__device__ __forceinline__ bool weigh(const float (&s)[2][4], float sc, const References<NG>& ref, const S (&vs)[2], half8 (&w)[NG], float& sum) {
     unsigned x[NG][4];
-    const float M_odd = M + 4.0f;
+    const float M = ref.M, M_odd = M + 4.0f;
+    float factor[NG];
+    if constexpr (!PLAIN) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) factor[g] = ldexpf(1.0f, ref.distance(g));
+    }
     sum = 0.0f;
     auto one = [&](auto R) {
         constexpr int r = decltype(R)::value;
@@ -255,7 +331,12 @@ __device__ __forceinline__ bool weigh(const float (&s)[2][4], float sc, float M,
             if constexpr (g < NG) {
                 typedef float f2 __attribute__((ext_vector_type(2)));
                 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-                const f2 y = {__builtin_fmaf(p[0], (float)half_of(vs[0][at / 2], at & 1), 0.0f), __builtin_fmaf(p[1], (float)half_of(vs[1][at / 2], at & 1), 0.0f)};
+                float a = p[0], b = p[1];
+                if constexpr (!PLAIN) {
+                    a *= factor[g];
+                    b *= factor[g];
+                }
+                const f2 y = {__builtin_fmaf(a, (float)half_of(vs[0][at / 2], at & 1), 0.0f), __builtin_fmaf(b, (float)half_of(vs[1][at / 2], at & 1), 0.0f)};
                 x[g][r] = __builtin_bit_cast(unsigned, __builtin_convertvector(y, h2));
             }
         };
@@ -277,22 +358,6 @@ __device__ __forceinline__ bool weigh(const float (&s)[2][4], float sc, float M,
     }
     return __builtin_amdgcn_ballot_w64(sum > P_LIMIT || half_of(top, 0) > W_LIMIT || half_of(top, 1) > W_LIMIT) != 0ull;
 }
-// the reference that a lane's 8 keys ask for
-template <int NG, class S>
-__device__ __forceinline__ float reference(const float (&s)[2][4], float sc, const S (&vs)[2]) {
-    float most = -__builtin_inff();
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            float scale = SMALLEST;
-#pragma unroll
-            for (int g = 0; g < NG; ++g) scale = __builtin_fmaxf(scale, (float)half_of(vs[j][(r * NG + g) / 2], (r * NG + g) & 1));
-            most = __builtin_fmaxf(most, __builtin_fmaf(s[j][r], sc, __builtin_amdgcn_logf(scale) - RAISE));
-        }
-    return most;
-}
-
 __device__ __forceinline__ void wave_order() {       // LDS written by other lanes of the wavefront: in program order
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -311,6 +376,27 @@ __device__ __forceinline__ float over_h(float x, bool sum) {
     x = sum ? x + y : __builtin_fmaxf(x, y);
     const float z = __shfl_xor(x, 32, 64);
     return sum ? x + z : __builtin_fmaxf(x, z);
+}
+// All references of a row raised to what the 32 keys of a lane and the three others of its column ask for, the sums l and O with them.
+template <int NG, int CT, class S>
+__device__ __forceinline__ void raise_references(const float (&s)[2][4], float sc, const S (&vs)[2], References<NG>& ref, const EmptyGroups<NG>& groups, float& l,
+                                                 c4f (&o)[CT]) {
+    float most[NG], alpha[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        most[g] = -__builtin_inff();
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float scale = __builtin_fmaxf(SMALLEST, (float)half_of(vs[j][(r * NG + g) / 2], (r * NG + g) & 1));
+                most[g] = __builtin_fmaxf(most[g], __builtin_fmaf(s[j][r], sc, __builtin_amdgcn_logf(scale) - RAISE));
+            }
+        most[g] = over_h(most[g], false);
+    }
+    l *= ref.raise(most, groups, alpha);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) o[ct] *= alpha[ct * NG / CT];
 }
 }  // namespace
 
@@ -387,6 +473,10 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
     constexpr int MERGE = WAVES * CT * 64 * 16, STAGE = WAVES * (int)sizeof(Lds);
     __shared__ __attribute__((aligned(16))) unsigned char lds[MERGE > STAGE ? MERGE : STAGE];
     __shared__ float s_m[WAVES][16], s_l[WAVES][16];
+    // (32 rows and four scales of 128 channels: no registers for the second tile's queries, which all wavefronts have alike, nor for
+    // addresses from one tile to the next)
+    constexpr bool STAGED = QT == 2 && NG * D == 512;
+    __shared__ half8 s_query[STAGED ? D / 32 : 1][64];
     const unsigned thousand = thousands();
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
     const RowsPlace at(c, q, tiles, n_splits);
@@ -400,7 +490,8 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
     if (part != nullptr && k_begin >= last_end) return;              // (the merge knows)
 
     Queries4<D> query[QT];
-    float sc[QT], M[QT], l[QT];
+    float sc[QT], l[QT];
+    References<NG> ref[QT];
     int end[QT];
     c4f o[QT][CT];
 #pragma unroll
@@ -408,12 +499,19 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
         const int row = row0 + min(16 * i + col, max(there - 1, 0)), tq = row / share, g = row - tq * share;
         sc[i] = query[i].load(q, b * q.strides.b + (head * share + g) * q.strides.h + tq * q.strides.n, h);
         end[i] = range.end(tq, q.causal);
-        M[i] = UNSET;
+        ref[i].clear();
         l[i] = 0.0f;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) o[i][ct] = (c4f){0.0f, 0.0f, 0.0f, 0.0f};
     }
 
+    if constexpr (STAGED) {
+        if (wave == 0) {
+#pragma unroll
+            for (int n = 0; n < D / 32; ++n) s_query[n][lane] = query[1].op[n];
+        }
+        __syncthreads();
+    }
     Lds& mine = *(Lds*)(lds + wave * sizeof(Lds));
     const int* const table = c.table + (size_t)b * c.columns;
     const unsigned char* const head_at = c.data + (size_t)head * c.block_bytes;
@@ -428,20 +526,24 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
         tile.request(c, head_at, pages, k0, lane);
         pages.look_up(c, table, k0 + NEXT);
     }
+    EmptyGroups<NG> groups;
+    bool plain = true;                  // the wavefront's rows have nothing but M
     for (; k0 < k_end; k0 += NEXT) {
         wave_order();
         // ---- the tile to LDS.  The scales of a row past the last key are perhaps no numbers: 0 instead.
         const unsigned bad = tile.bad;
         const bool absent = k0 + lane >= last_end || (bad >> h & 1);
         *(typename Tile::scale_t*)(mine.ks + lane * NG) = absent ? (typename Tile::scale_t)(0) : tile.ks;
-        *(typename Tile::scale_t*)(mine.vs + lane * NG) = absent ? (typename Tile::scale_t)(0) : tile.vs;
+        const typename Tile::scale_t v_scale = absent ? (typename Tile::scale_t)(0) : tile.vs;
+        *(typename Tile::scale_t*)(mine.vs + lane * NG) = v_scale;
+        if (NG > 1 && groups.empty != 0 && groups.look(v_scale)) plain = false;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) *(c4u*)(mine.v + v_chunk<D>((i * 1024 + lane * 16) / (D / 2), lane % (D / 32))) = tile.v[i];
 #pragma unroll
         for (int j = 0; j < 4; ++j) ((words*)mine.k)[j * 64 + lane] = tile.k[j];
         wave_order();
         if (k0 + NEXT < k_end) {
-            tile.request(c, head_at, pages, k0 + NEXT, lane);
+            tile.request(c, head_at, pages, k0 + NEXT, STAGED ? anew(lane) : lane);
             pages.look_up(c, table, k0 + 2 * NEXT);
         }
         const int v_key = 16 * (col >> 2) + 4 * h + (col & 3);
@@ -463,8 +565,10 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
                     for (int n = 0; n < STEPS; ++n) {
                         const half8 k = operand(kw[g * STEPS + n], thousand);
 #pragma unroll
-                        for (int i = 0; i < QT; ++i)
-                            a[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, query[i].op[g * STEPS + n], n == 0 ? (c4f){0.0f, 0.0f, 0.0f, 0.0f} : a[i], 0, 0, 0);
+                        for (int i = 0; i < QT; ++i) {
+                            const half8 row = STAGED && i == 1 ? s_query[g * STEPS + n][lane] : query[i].op[g * STEPS + n];
+                            a[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, row, n == 0 ? (c4f){0.0f, 0.0f, 0.0f, 0.0f} : a[i], 0, 0, 0);
+                        }
                     }
 #pragma unroll
                     for (int i = 0; i < QT; ++i)
@@ -487,23 +591,22 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
                     }
             }
             half8 w[QT][NG];
+            const bool again = !plain;
             // (no reference yet: no need to weigh twice, 2 us of 30 where a wavefront has one tile.  One tile of rows has no registers for the
             // branch: 108 us instead of 135)
             const bool first = QT > 1 && u == 0 && k0 == k_begin + TILE * wave;
 #pragma unroll
             for (int i = 0; i < QT; ++i) {
                 float sum;
-                if (first || weigh<NG>(s[i], sc[i], M[i], vs, w[i], sum)) {
-                    const float M_new = __builtin_fmaxf(M[i], over_h(reference<NG>(s[i], sc[i], vs), false));
-                    const float alpha = __builtin_amdgcn_exp2f(M[i] - M_new);
-                    M[i] = M_new;
-                    l[i] *= alpha;
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) o[i][ct] *= alpha;
-                    weigh<NG>(s[i], sc[i], M[i], vs, w[i], sum);
+                if (first || weigh<true, NG>(s[i], sc[i], ref[i], vs, w[i], sum) || again) {
+                    const scales_t own[2] = {anew(vs[0]), anew(vs[1])};
+                    raise_references<NG>(s[i], sc[i], own, ref[i], groups, l[i], o[i]);
+                    plain = ref[0].alike() && ref[QT - 1].alike();
+                    weigh<NG == 1, NG>(s[i], sc[i], ref[i], vs, w[i], sum);
                 }
                 l[i] += sum;
             }
+            groups.fresh = 0;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 // V transposed: channel 16 ct + lane % 16, nibble i of the words: key 16 (i / 4) + 4 h + i % 4
@@ -522,7 +625,7 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
         const float lw = over_h(l[i], true);
         __syncthreads();                // the tiles, or the query tile before, have been read
         if (h == 0) {
-            s_m[wave][col] = M[i];
+            s_m[wave][col] = ref[i].M;
             s_l[wave][col] = lw;
         }
         __syncthreads();
@@ -531,9 +634,9 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
         for (int w = 1; w < WAVES; ++w) top = __builtin_fmaxf(top, s_m[w][col]);
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) total = __builtin_fmaf(s_l[w][col], __builtin_amdgcn_exp2f(s_m[w][col] - top), total);
-        const float f = __builtin_amdgcn_exp2f(M[i] - top);
+        const float f = __builtin_amdgcn_exp2f(ref[i].M - top);
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) *(c4f*)(lds + ((wave * CT + ct) * 64 + lane) * 16) = o[i][ct] * f;
+        for (int ct = 0; ct < CT; ++ct) *(c4f*)(lds + ((wave * CT + ct) * 64 + lane) * 16) = o[i][ct] * (f * ref[i].back(ct * NG / CT));
         __syncthreads();
         const int row = row0 + 16 * i + col;
         if (row >= all_rows) continue;
@@ -590,7 +693,9 @@ cache4_attn_few_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStri
     if (part != nullptr && k_begin >= last_end) return;              // (the merge knows)
 
     half8 query[4][D / 32];
-    float sc, M = UNSET, l = 0.0f;
+    float sc, l = 0.0f;
+    References<NG> ref;
+    ref.clear();
     int end;
     {
         const int row = min(own, max(range.rows - 1, 0)), tq = row / share, g = row - tq * share;
@@ -630,13 +735,17 @@ cache4_attn_few_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStri
         tile.request(c, head_at, pages, k0, lane);
         pages.look_up(c, table, k0 + NEXT);
     }
+    EmptyGroups<NG> groups;
+    bool plain = true;                  // the wavefront's rows have nothing but M
     for (; k0 < k_end; k0 += NEXT) {
         wave_order();
         // ---- the tile to LDS.  The scales of a row past the last key are perhaps no numbers: 0 instead.
         const unsigned bad = tile.bad;
         const bool absent = k0 + lane >= last_end || (bad >> h & 1);
         *(typename Tile::scale_t*)(mine.ks + lane * NG) = absent ? (typename Tile::scale_t)(0) : tile.ks;
-        *(typename Tile::scale_t*)(mine.vs + lane * NG) = absent ? (typename Tile::scale_t)(0) : tile.vs;
+        const typename Tile::scale_t v_scale = absent ? (typename Tile::scale_t)(0) : tile.vs;
+        *(typename Tile::scale_t*)(mine.vs + lane * NG) = v_scale;
+        if (NG > 1 && groups.empty != 0 && groups.look(v_scale)) plain = false;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) *(c4u*)(mine.v + v_chunk<D>((i * 1024 + lane * 16) / (D / 2), lane % (D / 32))) = tile.v[i];
 #pragma unroll
@@ -674,46 +783,51 @@ cache4_attn_few_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStri
         // ---- weights, as weigh() forms them: two keys to a register
         unsigned x[NG][2];
         float sum;
-        auto weights = [&] {
+        auto weights = [&](auto P) {
+            constexpr bool PLAIN = decltype(P)::value;
             typedef float f2 __attribute__((ext_vector_type(2)));
             typedef _Float16 h2 __attribute__((ext_vector_type(2)));
             float p[4];
             sum = 0.0f;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, r & 1 ? -(M + 4.0f) : -M));
+                p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, r & 1 ? -(ref.M + 4.0f) : -ref.M));
                 sum = r & 1 ? __builtin_fmaf(p[r], 16.0f, sum) : sum + p[r];
             }
             unsigned top = 0;
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
+                const float factor = PLAIN ? 1.0f : ldexpf(1.0f, ref.distance(g));
 #pragma unroll
                 for (int r = 0; r < 4; r += 2) {
-                    const f2 y = {__builtin_fmaf(p[r], (float)half_of(vs[(r * NG + g) / 2], (r * NG + g) & 1), 0.0f),
-                                  __builtin_fmaf(p[r + 1], (float)half_of(vs[((r + 1) * NG + g) / 2], ((r + 1) * NG + g) & 1), 0.0f)};
+                    const float even = PLAIN ? p[r] : p[r] * factor, odd = PLAIN ? p[r + 1] : p[r + 1] * factor;
+                    const f2 y = {__builtin_fmaf(even, (float)half_of(vs[(r * NG + g) / 2], (r * NG + g) & 1), 0.0f),
+                                  __builtin_fmaf(odd, (float)half_of(vs[((r + 1) * NG + g) / 2], ((r + 1) * NG + g) & 1), 0.0f)};
                     x[g][r / 2] = __builtin_bit_cast(unsigned, __builtin_convertvector(y, h2));
                 }
                 top = max3_pairs(top, x[g][0], x[g][1]);
             }
             return __builtin_amdgcn_ballot_w64(sum > P_LIMIT || half_of(top, 0) > W_LIMIT || half_of(top, 1) > W_LIMIT) != 0ull;
         };
-        if (__builtin_expect(weights(), 0)) {
-            float most = -__builtin_inff();
+        if (__builtin_expect(weights(std::true_type{}) || !plain, 0)) {
+            float most[NG], alpha[NG];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float scale = SMALLEST;
+            for (int g = 0; g < NG; ++g) {
+                most[g] = -__builtin_inff();
 #pragma unroll
-                for (int g = 0; g < NG; ++g) scale = __builtin_fmaxf(scale, (float)half_of(vs[(r * NG + g) / 2], (r * NG + g) & 1));
-                most = __builtin_fmaxf(most, __builtin_fmaf(s[r], sc, __builtin_amdgcn_logf(scale) - RAISE));
+                for (int r = 0; r < 4; ++r) {
+                    const float scale = __builtin_fmaxf(SMALLEST, (float)half_of(vs[(r * NG + g) / 2], (r * NG + g) & 1));
+                    most[g] = __builtin_fmaxf(most[g], __builtin_fmaf(s[r], sc, __builtin_amdgcn_logf(scale) - RAISE));
+                }
+                most[g] = __builtin_fmaxf(most[g], __shfl_xor(most[g], 4, 64));
+                most[g] = over_h(__builtin_fmaxf(most[g], __shfl_xor(most[g], 8, 64)), false);
             }
-            most = __builtin_fmaxf(most, __shfl_xor(most, 4, 64));
-            most = __builtin_fmaxf(most, __shfl_xor(most, 8, 64));
-            const float M_new = __builtin_fmaxf(M, over_h(most, false)), alpha = __builtin_amdgcn_exp2f(M - M_new);
-            M = M_new;
-            l *= alpha;
+            l *= ref.raise(most, groups, alpha);
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) o[ct] *= alpha;
-            weights();
+            for (int ct = 0; ct < CT; ++ct) o[ct] *= alpha[ct * NG / CT];
+            plain = ref.alike();
+            groups.fresh = 0;
+            weights(std::integral_constant<bool, NG == 1>{});
         }
         l += sum;
         half8 w[2][NG];
@@ -739,7 +853,7 @@ cache4_attn_few_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStri
     const float lw = over_fours(over_h(l, true));
     __syncthreads();                    // the tiles have been read
     if (lane < 4) {
-        s_m[wave][own] = M;
+        s_m[wave][own] = ref.M;
         s_l[wave][own] = lw;
     }
     __syncthreads();
@@ -748,12 +862,12 @@ cache4_attn_few_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStri
     for (int w = 1; w < WAVES; ++w) top = __builtin_fmaxf(top, s_m[w][own]);
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) total = __builtin_fmaf(s_l[w][own], __builtin_amdgcn_exp2f(s_m[w][own] - top), total);
-    const float f = __builtin_amdgcn_exp2f(M - top);
+    const float f = __builtin_amdgcn_exp2f(ref.M - top);
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
         c4f x;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = over_fours(o[ct][r]) * f;
+        for (int r = 0; r < 4; ++r) x[r] = over_fours(o[ct][r]) * (f * ref.back(ct * NG / CT));
         if (piece == 0) *(c4f*)(lds + ((wave * CT + ct) * 16 + 4 * h + own) * 16) = x;
     }
     __syncthreads();
@@ -848,7 +962,8 @@ cache4_attn_rows_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStr
     if (part != nullptr && k_begin >= last_end) return;              // (the merge knows)
 
     Queries4<D> query[QT];
-    float sc[QT], M[QT], l[QT];
+    float sc[QT], l[QT];
+    References<NG> ref[QT];
     int end[QT];
     c4f o[QT][CT];
 #pragma unroll
@@ -856,7 +971,7 @@ cache4_attn_rows_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStr
         const int row = min(row0 + 16 * i + col, max(range.rows - 1, 0)), tq = row / share, g = row - tq * share;
         sc[i] = query[i].load(q, b * q.strides.b + (head * share + g) * q.strides.h + tq * q.strides.n, h);
         end[i] = range.end(tq, q.causal);
-        M[i] = UNSET;
+        ref[i].clear();
         l[i] = 0.0f;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) o[i][ct] = (c4f){0.0f, 0.0f, 0.0f, 0.0f};
@@ -945,23 +1060,24 @@ cache4_attn_rows_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStr
                     if (k0 + 16 * (2 * u + j) + 4 * h + r >= last) x.s[i][j][r] = -__builtin_inff();
             }
     };
-    auto weighed = [&](Half& x) {
+    EmptyGroups<NG> groups;
+    bool plain = true;                  // the wavefront's rows have nothing but M
+    auto weighed = [&](Half& x, auto P) {
         bool low = false;
 #pragma unroll
-        for (int i = 0; i < QT; ++i) low |= weigh<NG>(x.s[i], sc[i], M[i], x.vs, x.w[i], x.sum[i]);
+        for (int i = 0; i < QT; ++i) low |= weigh<decltype(P)::value, NG>(x.s[i], sc[i], ref[i], x.vs, x.w[i], x.sum[i]);
         return low;
     };
-    auto raise = [&](Half& x) {
+    // the references are too low, or groups have references of their own, which may be too low as well
+    auto again = [&](Half& x) {
 #pragma unroll
         for (int i = 0; i < QT; ++i) {
-            const float M_new = __builtin_fmaxf(M[i], over_h(reference<NG>(x.s[i], sc[i], x.vs), false));
-            const float alpha = __builtin_amdgcn_exp2f(M[i] - M_new);
-            M[i] = M_new;
-            l[i] *= alpha;
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) o[i][ct] *= alpha;
-            weigh<NG>(x.s[i], sc[i], M[i], x.vs, x.w[i], x.sum[i]);
+            const scales_t own[2] = {anew(x.vs[0]), anew(x.vs[1])};
+            raise_references<NG>(x.s[i], sc[i], own, ref[i], groups, l[i], o[i]);
         }
+        plain = ref[0].alike() && ref[QT - 1].alike();
+        groups.fresh = 0;
+        weighed(x, std::integral_constant<bool, NG == 1>{});
     };
     auto values = [&](const Half& x, const TileStage<D, NG>& now, int u) {
 #pragma unroll
@@ -980,15 +1096,16 @@ cache4_attn_rows_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStr
         if (k0 < wave_end) {
             // products of one half beside the other half's weights
             const bool masked = k0 + TILE > first_end || now_bad != 0;
+            if (NG > 1 && groups.empty != 0 && groups.look(((const typename ScaleWord<NG>::type*)now.vs)[lane])) plain = false;
             if constexpr (NG <= 2) {
                 Half x, y;
                 score(x, now, 0);
                 if (masked) hide(x, k0, 0);
                 score(y, now, 1);
-                if (__builtin_expect(weighed(x), 0)) raise(x);
+                if (__builtin_expect(weighed(x, std::true_type{}) || !plain, 0)) again(x);
                 if (masked) hide(y, k0, 1);
                 values(x, now, 0);
-                if (__builtin_expect(weighed(y), 0)) raise(y);
+                if (__builtin_expect(weighed(y, std::true_type{}) || !plain, 0)) again(y);
                 values(y, now, 1);
             } else {
                 // (four groups' operands and scales: no registers for two halves)
@@ -997,7 +1114,7 @@ cache4_attn_rows_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStr
                     Half x;
                     score(x, now, u);
                     if (masked) hide(x, k0, u);
-                    if (__builtin_expect(weighed(x), 0)) raise(x);
+                    if (__builtin_expect(weighed(x, std::true_type{}) || !plain, 0)) again(x);
                     values(x, now, u);
                 }
             }
@@ -1017,10 +1134,10 @@ cache4_attn_rows_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStr
         const float total = over_h(l[i], true);
         const int row = row0 + 16 * i + col;
         if (row >= all_rows) continue;
-        const RowResult r(at, q, head, share, row, row < range.rows, M[i], total, all_rows);
+        const RowResult r(at, q, head, share, row, row < range.rows, ref[i].M, total, all_rows);
         if (h == 0) r.put_sum(q, lse, part_lse, part != nullptr);
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) r.template put<D>(q, out, os, part, o[i][ct], 16 * ct + 4 * h);
+        for (int ct = 0; ct < CT; ++ct) r.template put<D>(q, out, os, part, o[i][ct] * ref[i].back(ct * NG / CT), 16 * ct + 4 * h);
     }
 }
 
