@@ -23,6 +23,23 @@ template <> struct RopeType<float> {
     static __device__ __forceinline__ float put(float x) { return x; }
 };
 
+// Sine and cosine of a number of turns, times amplitude (the sine also times sign): the fraction is what counts, in fp64, as far positions are
+// many turns.  Rounded to fp32 it is off by up to 2^-26 of a turn, 9e-8 of an angle: next to nothing beside a 16-bit type's step.  In fp32
+// that would be half of a result's error, so there the rest is put back, by the first two terms of the sum of two angles.
+template <class T>
+__device__ __forceinline__ void turn_of(double turns, float amplitude, float sign, float& c, float& s) {
+    const double fraction = turns - __builtin_rint(turns);
+    const float near = (float)fraction;
+    sincospif(2.0f * near, &s, &c);
+    if constexpr (sizeof(T) == 4) {
+        const float rest = (float)(fraction - near) * 6.2831853071795865f, c0 = c;
+        c = __builtin_fmaf(-rest, s, c);
+        s = __builtin_fmaf(rest, c0, s);
+    }
+    c *= amplitude;
+    s *= sign * amplitude;
+}
+
 // VEC pairs of a token for HEADS heads: both halves of the pairs as vectors of 8 bytes (interleaved: 2 VEC neighbouring channels),
 // the angles made once for all heads while the rows are on their way.  Vectors past the rotated channels are copied.  168 MB read
 // and written (2 x 4096 tokens, 40 heads of 128, bf16) take 34-36 us, 4.7-4.9 TB/s, a copy of 1 GiB reaches 5.2; with vectors of
@@ -57,13 +74,7 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeTensor q, RopeTensor k, c
         float c[VEC], s[VEC];
         const double position = positions[b * position_stride + n] * 0.15915494309189535;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            // turns, in fp64: far positions are many of them, and only the fraction counts
-            const double turns = position * inv_freq[VEC * j + e];
-            sincospif(2.0f * (float)(turns - __builtin_rint(turns)), &s[e], &c[e]);
-            c[e] *= amplitude;
-            s[e] *= sign * amplitude;
-        }
+        for (int e = 0; e < VEC; ++e) turn_of<T>(position * inv_freq[VEC * j + e], amplitude, sign, c[e], s[e]);
 #pragma unroll
         for (int i = 0; i < HEADS; ++i) {
             if (interleaved) {
@@ -120,11 +131,8 @@ __global__ void __launch_bounds__(256) rope_pair_kernel(RopeTensor q, RopeTensor
         y[2 * i + 1] = v;
         return;
     }
-    const double turns = positions[b * position_stride + n] * 0.15915494309189535 * inv_freq[i];
     float s, c;
-    sincospif(2.0f * (float)(turns - __builtin_rint(turns)), &s, &c);
-    c *= amplitude;
-    s *= sign * amplitude;
+    turn_of<T>(positions[b * position_stride + n] * 0.15915494309189535 * inv_freq[i], amplitude, sign, c, s);
     const int c0 = interleaved ? 2 * i : i, c1 = interleaved ? 2 * i + 1 : i + R / 2;
     const float u = RopeType<T>::get(x[c0]), v = RopeType<T>::get(x[c1]);
     y[c0] = RopeType<T>::put(u * c - v * s);
