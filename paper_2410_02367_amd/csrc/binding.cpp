@@ -9,6 +9,7 @@
 // The interpreter lock is released around the library calls, as ctypes does.
 #include <Python.h>
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -444,6 +445,8 @@ template <bool BWD> PyObject* py_rope(PyObject* const* argv, Py_ssize_t n) {
     const float amplitude = a.real();
     const at::Tensor *gq = a.rows_or_none(true), *gk = a.rows_or_none(true);
     void* st = a.stream();
+    // (calls that autograd takes note of are serving.py's)
+    if (at::GradMode::is_enabled() && a.ok && (q->requires_grad() || (k && k->requires_grad()) || freq->requires_grad())) return none();
     if (!a.take(gq && (gk || !k)) || (gk && !k)) return none();
     LikeBuffer oq, ok;
     if (!oq.take_like(gq, argv[6], *q) || (k && !ok.take_like(gk, argv[7], *k))) return none();

@@ -168,6 +168,7 @@ def _rope(entry, x, y, positions, inv_freq, interleaved, amplitude, x_out, y_out
 
 
 def _tracked(*tensors) -> bool:
+    """Whether autograd takes note of a call (the extension module, which asks the same, leaves such calls to the code here)."""
     return any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors) and torch.is_grad_enabled()
 
 
@@ -220,22 +221,22 @@ def sage_rope(q, k, positions, inv_freq, interleaved: bool = False, amplitude: f
     """q [B,Hq,N,D] and k [B,Hk,N,D] (or None) with their pairs of channels turned by position * inv_freq -> (q', k'), or q'.
     positions int32 [N] or [B,N]; inv_freq fp64 [rotated / 2], the channels from `rotated` on pass; outputs may be the inputs.
     Differentiable in q and k, where no output is given: the gradients are sage_rope_bwd()'s."""
-    if _tracked(q, k, inv_freq):
-        return _turn(False, q, k, positions, inv_freq, interleaved, amplitude, q_out, k_out, stream)
     r = _fast().rope(q, k, positions, inv_freq, interleaved, amplitude, q_out, k_out, _handle(stream))
     if r is not None:
         return _answer(r, "sage_rope")
+    if _tracked(q, k, inv_freq):
+        return _turn(False, q, k, positions, inv_freq, interleaved, amplitude, q_out, k_out, stream)
     return _rope("sage_rope", q, k, positions, inv_freq, interleaved, amplitude, q_out, k_out, stream)
 
 
 def sage_rope_bwd(dq, dk, positions, inv_freq, interleaved: bool = False, amplitude: float = 1.0, dq_out=None, dk_out=None, stream=None):
     """The gradients of sage_rope()'s inputs from those of its outputs, dq [B,Hq,N,D] and dk [B,Hk,N,D] (or None).  Differentiable as
     that is."""
-    if _tracked(dq, dk, inv_freq):
-        return _turn(True, dq, dk, positions, inv_freq, interleaved, amplitude, dq_out, dk_out, stream)
     r = _fast().rope_bwd(dq, dk, positions, inv_freq, interleaved, amplitude, dq_out, dk_out, _handle(stream))
     if r is not None:
         return _answer(r, "sage_rope_bwd")
+    if _tracked(dq, dk, inv_freq):
+        return _turn(True, dq, dk, positions, inv_freq, interleaved, amplitude, dq_out, dk_out, stream)
     return _rope("sage_rope_bwd", dq, dk, positions, inv_freq, interleaved, amplitude, dq_out, dk_out, stream)
 
 
