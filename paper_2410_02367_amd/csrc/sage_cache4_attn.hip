@@ -1462,8 +1462,8 @@ __global__ void __launch_bounds__(NW * 64, 2) cache4_weights_rows_kernel(Cache4 
     float sum[4] = {};
     unsigned bad = 0;
     int row0 = 16 * wave;
-    // (of the first rows those that see no key of the workgroup are passed over)
-    if (q.causal) row0 += max(0, k0 + 1 - (range.length - range.count + 1)) * share / (16 * NW) * (16 * NW);
+    // (of the first rows those that see no key of the workgroup are passed over; where some row sees one they are fewer than all)
+    if (q.causal && k0 < last_end) row0 += max(0, k0 + 1 - (range.length - range.count + 1)) * share / (16 * NW) * (16 * NW);
     if (k0 < last_end && row0 < range.rows) {
         half8 k[4][D / 32];
         LaneScales<NG> ks[4];
