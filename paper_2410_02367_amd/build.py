@@ -378,16 +378,32 @@ def check_no_spills(text: str) -> list:
     return problems
 
 
+def _loops(lines: list) -> list:
+    """(first, last) line of every loop of a kernel's text: from a label to the last branch back to it."""
+    import re
+    labels, loops = {}, {}
+    for i, line in enumerate(lines):
+        label = re.match(r"(\.LBB\w+):", line)
+        if label:
+            labels[label.group(1)] = i
+        target = re.match(r"\s*s_c?branch\w*\s+(\.LBB\w+)", line)
+        if target and target.group(1) in labels:
+            loops[labels[target.group(1)]] = i
+    return sorted(loops.items())
+
+
 def check_cache4_attn_asm(text: str) -> list:
-    """The kernels over the 4-bit cache, between a kernel's first matrix instruction and its last, which is the walk over the keys: no
-    scratch access (at the walk's head the kernel with 32 rows and four scales per key reads two addresses back), and no line
-    of inline assembly, whose registers the compiler would not keep apart from those of a matrix instruction still under way."""
+    """The kernels over the 4-bit cache, in the walk over the keys, that is between a kernel's first matrix instruction and its last and in
+    all of every loop that holds one: no scratch access, and no line of inline assembly, whose registers the compiler would not keep
+    apart from those of a matrix instruction still under way (over a loop's back edge as well)."""
     import re
     problems = []
     for m in re.finditer(r"^(_ZN4sage\w+):.*?^\.Lfunc_end\d+:", text, re.S | re.M):
         lines = m.group(0).split("\n")
         products = [i for i, line in enumerate(lines) if "v_mfma" in line]
-        walk = lines[products[0]:products[-1]] if products else lines
+        parts = [(products[0], products[-1])] if products else [(0, len(lines) - 1)]
+        parts += [(first, last) for first, last in _loops(lines) if any(first <= i <= last for i in products)]
+        walk = [line for i, line in enumerate(lines) if any(first <= i <= last for first, last in parts)]
         if any("scratch_" in line for line in walk):
             problems.append(f"{m.group(1)}: scratch access (register spill)")
         written = "\n".join(line for line in walk if line.strip())
