@@ -26,7 +26,8 @@
 // 2^8 times the others, 116 -> 192 with 16 rows, 915 -> 2580 for 1024 queries of 32 heads on 32K keys.  (A product with a power of two
 // per row and group in any case: 719 us for 717 for those 1024 with two groups, 979 for 915 with four, 119 for 116 with the 16 rows.)
 // The weights in fp16 are a choice: with half a step of 2^-11 each they take the error of an fp16 output against 64 bits from 2.1e-4, its own
-// rounding, to 2.9e-4.  The sums l (with M) and O (each group with its R) are fp32.
+// rounding, to 2.9e-4 (a bf16 output's stays 1.7e-3).  With what the rounding leaves as a second operand it is 2.1e-4 again, at 109 us for 102
+// for a decoding step of 32 sequences and at 1014 for 715 for 1024 queries on 32K keys.  The sums l (with M) and O (each group with its R) are fp32.
 #include "sage_serving.h"
 #include "sage_device.h"
 
