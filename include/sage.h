@@ -470,7 +470,8 @@ int sage_cache4_load(const void* cache, const int32_t* pages, const int32_t* sta
 /*
  * Attention of new queries over the cache, softmax(sm_scale q K^T) V with K and V as the cache holds them: FP16 products of the
  * codes with fp32 accumulation (q is not quantized), the scales applied to the sums; a weight times a scale of V is rounded to
- * fp16 for the second product.  Query head hq reads key head hq / (Hq / Hkv).  Scores up to 2^25 (in the exponent of 2).  A query
+ * fp16 for the second product, relative to the largest such product of its group of channels (2^-11 of itself, or 2^-23 of that one
+ * where this is more), whatever the other groups' are.  Query head hq reads key head hq / (Hq / Hkv).  Scores up to 2^25 (in the exponent of 2).  A query
  * that is no number leaves the others alone.
  *   q        in   [B,Hq,Nq,D] SAGE_F16 or SAGE_BF16;  out  out, the same type and shape, fully overwritten
  *   lengths  in   [B] int32: tokens of the sequence in the cache (the queries' own among them); limited to 0 .. columns * page
@@ -482,7 +483,8 @@ int sage_cache4_load(const void* cache, const int32_t* pages, const int32_t* sta
  *   n_splits   how many workgroups share a row's keys (at most the table's tokens / 256), 0: chosen from the shape
  *   workspace  device, >= sage_cache4_attn_workspace() bytes (same arguments), 16-byte aligned; scratch, contents undefined
  *              on entry and exit; may be NULL when that size is 0.  Two calls that share one are ordered by the caller
- *   A call of 2^24 workgroups and more is refused (SAGE_ERR_SHAPE)
+ *   A call of 2^24 workgroups and more is refused (SAGE_ERR_SHAPE).  Keys are shared out by the table's columns, as lengths are not known on
+ *   the host: with a table much wider than the sequences few workgroups have work (n_splits sets how many there are)
  */
 size_t sage_cache4_attn_workspace(int B, int Hq, int Hkv, int Nq, int D, int columns, int page, int n_splits);
 int sage_cache4_attn(const void* q, const int64_t* q_strides, const void* cache, const int32_t* pages, const int32_t* lengths,
@@ -498,7 +500,7 @@ int sage_cache4_attn(const void* q, const int64_t* q_strides, const void* cache,
  *   lse      in   from sage_cache4_attn with the same arguments (a row whose lse is -infinity adds nothing, one whose lse is
  *            no number makes its keys' sums NaN).  The weights of a row sum to 1
  *   weights  in   [B,Hkv,width] fp32, or NULL: zeros;  out  out, the same shape, may be weights itself; width >= columns * page.
- *            Slots from lengths[b] on keep their value
+ *            Slots from lengths[b] on keep their value.  All of the width is read and written: the narrower, the faster
  */
 int sage_cache4_weights(const void* q, const int64_t* q_strides, const void* cache, const int32_t* pages, const int32_t* lengths,
                         const int32_t* count, const float* lse, const float* weights, float* out, int width,

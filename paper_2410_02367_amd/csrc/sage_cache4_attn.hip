@@ -670,9 +670,9 @@ __device__ __forceinline__ float over_fours(float x) {
 // With four rows a quarter of the score products' columns would be of use.  Column 4 j + c of them is row c for the keys of piece j: the
 // queries of piece j's product are zero in the other columns, and the four products of a tile add up into one.  A lane has 4
 // scores per tile instead of 16 and weighs those; its weights stand, in its column of the second product, at the keys of its
-// piece beside zeros, and the columns of a row are added up at the end.  489 vector instructions per tile for 644; 256 slabs of 8K to 16K keys
-// of 128 channels 104 us for 119, the same loads alone 82.  (The queries in LDS, for three wavefronts per
-// SIMD instead of two: 104.)
+// piece beside zeros, and the columns of a row are added up at the end.  Some 490 vector instructions per tile for 650; 256 slabs of 8K to 16K
+// keys of 128 channels with four scales 108 us for 117, the same loads alone 82.  (The queries in LDS, for three wavefronts per
+// SIMD instead of two: no change.)
 template <int D, int NG>
 __global__ void __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2)
 cache4_attn_few_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides os, float* __restrict__ lse, float* __restrict__ part,
@@ -1525,8 +1525,9 @@ namespace {
 // 2048 keys at least, even that out (256 slabs of 8K to 16K keys: 2 chunks 117, 8 chunks 106; all of 16K: 126 and 122; 80 of 18K to 36K
 // with 52 rows: 3 chunks 238, 12 chunks 190; 32 of 16K to 32K with 1024 rows: 2 chunks 729, 8 chunks 646; 16 of 8K to 16K with
 // 1024 rows: 4 chunks 195, 8 chunks 201).  Rows: 16 or 32 per workgroup, whose wavefronts share the keys; or 128, whose
-// wavefronts share the operands, where there are that many and the chunks are long (us with 32 / 128: 4096 rows of 8 slabs of 32K
-// keys 1117 / 934, of 4K 117 / 111, 128 rows of 64 slabs of 16K 125 / 108; chunks of 512 keys: 512 rows of 32 slabs of 2K 42 / 49).
+// wavefronts share the operands, where there are that many and the chunks are long (us with 32 / 128, four scales per key: 4096 rows of 8
+// slabs of 32K keys 1067 / 911, of 8K 270 / 253, of 4K 139 / 141, 2048 of 32 of 2K 151 / 131, 128 of 64 of 16K 170 / 140; chunks of 512
+// keys: 512 rows of 32 slabs of 2K 47 / 56).
 struct AttnPlan {
     int rows, tiles, n_splits, chunk;       // rows of a workgroup
 };

@@ -42,8 +42,9 @@ __device__ __forceinline__ void turn_of(double turns, float amplitude, float sig
 
 // VEC pairs of a token for HEADS heads: both halves of the pairs as vectors of 8 bytes (interleaved: 2 VEC neighbouring channels),
 // the angles made once for all heads while the rows are on their way.  Vectors past the rotated channels are copied.  168 MB read
-// and written (2 x 4096 tokens, 40 heads of 128, bf16) take 34-36 us, 4.7-4.9 TB/s, a copy of 1 GiB reaches 5.2; with vectors of
-// 16 bytes 44, with one head per thread 43-47; fp32, twice the bytes, 70 and 81.
+// and written (2 x 4096 tokens, 40 heads of 128, bf16) take 37-41 us, 4.1-4.6 TB/s, where a training step's tensors come from memory (a
+// copy of 1 GiB reaches 5.2), and 29 where the same ones are rotated again and again; fp32, twice the bytes, 72 there.  Beside 34-36 in
+// one comparison: vectors of 16 bytes 44, one head per thread 43-47.
 template <class T, int VEC, int HEADS>
 __global__ void __launch_bounds__(256) rope_kernel(RopeTensor q, RopeTensor k, const int* __restrict__ positions, long position_stride,
                                                    const double* __restrict__ inv_freq, float amplitude, int N, int D, int R,
