@@ -295,7 +295,9 @@ struct References {
         unsigned now = 0;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            const float d = M - R[g] <= ALIKE || (groups.empty >> g & 1) || R[g] == UNSET ? 0.0f : __builtin_fminf(M - R[g], FARTHEST);
+            // (a row that is no number has none either)
+            const bool own = M - R[g] > ALIKE && !(groups.empty >> g & 1) && R[g] != UNSET;
+            const float d = own ? __builtin_fminf(M - R[g], FARTHEST) : 0.0f;
             alpha[g] = __builtin_amdgcn_exp2f((M_old - M) + (d - (float)distance(g)));
             now |= (unsigned)d << 8 * g;
         }
