@@ -470,9 +470,9 @@ int sage_cache4_load(const void* cache, const int32_t* pages, const int32_t* sta
 /*
  * Attention of new queries over the cache, softmax(sm_scale q K^T) V with K and V as the cache holds them: FP16 products of the
  * codes with fp32 accumulation (q is not quantized), the scales applied to the sums; a weight times a scale of V is rounded to
- * fp16 for the second product, relative to the largest such product of its group of channels (2^-11 of itself, or 2^-23 of that one
- * where this is more), whatever the other groups' are.  Query head hq reads key head hq / (Hq / Hkv).  Scores up to 2^25 (in the exponent of 2).  A query
- * that is no number leaves the others alone.
+ * fp16 for the second product: off by 2^-11 of itself, or by 2^-23 of the largest such product of its row and group of channels,
+ * or 2^-100 of that of its row, whichever is most.  Query head hq reads key head hq / (Hq / Hkv).  Scores up to 2^25 (in the exponent of 2).  A query that is no
+ * number leaves the others alone.
  *   q        in   [B,Hq,Nq,D] SAGE_F16 or SAGE_BF16;  out  out, the same type and shape, fully overwritten
  *   lengths  in   [B] int32: tokens of the sequence in the cache (the queries' own among them); limited to 0 .. columns * page
  *   count    in   [B] int32, or NULL: Nq.  Sequence b has the queries t < count[b]; the rows behind them become zeros

@@ -19,12 +19,13 @@
 // What is rounded to fp16, a weight times its key's scale, is bounded by a reference R per row and group of channels: it is
 // exp2(s - R) * scale, and where one passes 2^15 (or the weights of 8 keys 2^50) R is raised to the largest s + log2(scale) less 10, rounded up
 // to a whole number.  So the range of fp16 is spent on what reaches the group's output, whatever the scales are: neither a key with large
-// values and next to no weight nor a group of larger values leaves others less precision.  M is the largest R of a row.  Groups that ask for
-// up to 7 less, or have had no value but 0, share it (their largest is 2^2 at least, so that what rounds to a subnormal number is off by 2^-23 of it), and as long
-// as all rows of a wavefront have nothing but M, which is the rule, a weight is one product.  Where they have not, 32 keys are weighed again with a
-// product more per group, and R follows the largest: 108 -> 127 us for 256 slabs of 8K to 16K keys with four rows and one group of four
-// 2^8 times the others, 116 -> 192 with 16 rows, 915 -> 2580 for 1024 queries of 32 heads on 32K keys.  (A product with a power of two
-// per row and group in any case: 719 us for 717 for those 1024 with two groups, 979 for 915 with four, 119 for 116 with the 16 rows.)
+// values and next to no weight nor a group of larger values leaves others less precision, down to 2^-100 of a row's largest, below which the
+// exponentials leave fp32.  M is the largest R of a row, and its largest s less 46 at least.  Groups that ask for up to 7 less, or have had
+// no value but 0, share it (their largest is 2^2 at least, so that what rounds to a subnormal number is off by 2^-23 of it), and as
+// long as all rows of a wavefront have nothing but M, which is the rule, a weight is one product.  Where they have not, 32 keys are weighed
+// again with a product more per group, and R follows the largest: 108 -> 129 us for 256 slabs of 8K to 16K keys with four rows and one group of
+// four 2^8 times the others, 118 -> 194 with 16 rows, 912 -> 2680 for 1024 queries of 32 heads on 32K keys.  (A product with a power of two
+// per row and group in any case: 719 us for 717 for those 1024 with two groups, 979 for 915 with four, 119 for 117 with the 16 rows.)
 // The weights in fp16 are a choice: with half a step of 2^-11 each they take the error of an fp16 output against 64 bits from 2.1e-4, its own
 // rounding, to 2.9e-4 (a bf16 output's stays 1.7e-3).  With what the rounding leaves as a second operand it is 2.1e-4 again, at 109 us for 102
 // for a decoding step of 32 sequences and at 1014 for 715 for 1024 queries on 32K keys.  The sums l (with M) and O (each group with its R) are fp32.
@@ -43,7 +44,7 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float UNSET = -1e30f;             // a reference below every score: the first key that is seen raises it
 constexpr _Float16 W_LIMIT = 32768.0f;
 constexpr float P_LIMIT = 0x1p50f;
-constexpr float RAISE = 10.0f, ALIKE = 7.0f, FARTHEST = 100.0f, SMALLEST = 0x1p-36f;
+constexpr float RAISE = 10.0f, ALIKE = 7.0f, FARTHEST = 120.0f, FLOOR = 46.0f;
 constexpr int TILE = 64, WAVES = 4, FEW_CHUNK = 2048;
 
 // 8 codes of a word -> operand registers: element 2 m + s is the code of nibble m + 4 s, times 16 where m is odd.  A nibble in the
@@ -250,11 +251,11 @@ __device__ __forceinline__ T anew(T x) {
     return x;
 }
 
-// Groups of a wavefront's keys, a bit each: those that had no value but 0 so far, and of those the ones that have one in the present tile.
-// (An empty group asks for no reference: channels that only fill up a head would have one of their own for nothing.)
+// Groups of a wavefront's keys that had no value but 0 so far, a bit each.  (Such a group asks for no reference: channels that only fill
+// up a head would have one of their own for nothing.)
 template <int NG>
 struct EmptyGroups {
-    unsigned empty = (1u << NG) - 1u, fresh = 0;
+    unsigned empty = (1u << NG) - 1u;
     // scales: those of the lane's key of a tile -> whether a group of them is no longer empty (the same in all lanes)
     template <class S>
     __device__ __forceinline__ bool look(S scales) {
@@ -266,46 +267,56 @@ struct EmptyGroups {
             else own = (unsigned short)(scales >> 16 * g);
             if (__builtin_amdgcn_ballot_w64((own & 0x7fff) != 0) != 0ull) seen |= 1u << g;
         }
-        fresh = empty & seen;
+        const unsigned fresh = empty & seen;
         empty &= ~seen;
         return fresh != 0;
     }
 };
-// The references of a row: M, and how far below it those of the groups are, whole numbers in 8 bits each.
+// The references of a row: M, and how far below it those of the groups are, whole numbers in 8 bits each; NONE: the row has seen no value
+// of the group but 0, so that the group's sums are 0.
 template <int NG>
 struct References {
+    static constexpr unsigned NONE = 255;
     float M;
     unsigned below;
     __device__ __forceinline__ void clear() {
         M = UNSET;
-        below = 0;
+        below = ~0u;
     }
-    __device__ __forceinline__ int distance(int g) const { return NG == 1 ? 0 : (int)(below >> 8 * g & 255u); }
+    __device__ __forceinline__ unsigned byte(int g) const { return below >> 8 * g & 255u; }
+    __device__ __forceinline__ int distance(int g) const { return NG == 1 || byte(g) == NONE ? 0 : (int)byte(g); }
     // what brings sums of group g to M
     __device__ __forceinline__ float back(int g) const { return ldexpf(1.0f, -distance(g)); }
-    // raised to what the row's keys ask for; alpha: what the groups' sums so far are multiplied by -> what l is (whole powers of two)
-    __device__ __forceinline__ float raise(const float (&most)[NG], const EmptyGroups<NG>& groups, float (&alpha)[NG]) {
+    // raised to what the row's keys ask for, M to their largest score less FLOOR at least, which bounds the sum of the weights; alpha: what the groups'
+    // sums so far are multiplied by -> what l is (whole powers of two)
+    __device__ __forceinline__ float raise(const float (&most)[NG], float score, float (&alpha)[NG]) {
         const float M_old = M;
         float R[NG];
+        M = __builtin_fmaxf(M, __builtin_ceilf(score - FLOOR));
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            R[g] = __builtin_fmaxf(groups.fresh >> g & 1 ? UNSET : M_old - (float)distance(g), __builtin_ceilf(most[g]));
+            R[g] = __builtin_fmaxf(NG > 1 && byte(g) == NONE ? UNSET : M_old - (float)distance(g), __builtin_ceilf(most[g]));
             M = __builtin_fmaxf(M, R[g]);
         }
         unsigned now = 0;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            // (a row that is no number has none either)
-            const bool own = M - R[g] > ALIKE && !(groups.empty >> g & 1) && R[g] != UNSET;
-            const float d = own ? __builtin_fminf(M - R[g], FARTHEST) : 0.0f;
+            // (a row that is no number has nothing but M)
+            const float d = NG > 1 && M - R[g] > ALIKE ? __builtin_fminf(M - R[g], FARTHEST) : 0.0f;
             alpha[g] = __builtin_amdgcn_exp2f((M_old - M) + (d - (float)distance(g)));
-            now |= (unsigned)d << 8 * g;
+            now |= (R[g] == UNSET ? NONE : (unsigned)d) << 8 * g;
         }
         below = now;
         return __builtin_amdgcn_exp2f(M_old - M);
     }
-    // whether the rows of the wavefront have nothing but M (the same in all lanes)
-    __device__ __forceinline__ bool alike() const { return NG == 1 || __builtin_amdgcn_ballot_w64(below != 0u) == 0ull; }
+    // whether the rows of the wavefront have nothing but M for the groups that are not empty (the same in all lanes)
+    __device__ __forceinline__ bool alike(const EmptyGroups<NG>& groups) const {
+        if constexpr (NG == 1) return true;
+        unsigned others = 0;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) others |= groups.empty >> g & 1 ? 0u : 255u << 8 * g;
+        return __builtin_amdgcn_ballot_w64((below & others) != 0u) == 0ull;
+    }
 };
 
 // The weights of 32 keys for 16 rows: register r of the two score tiles is keys 4 h + r and 16 + 4 h + r, element 2 r and 2 r + 1
@@ -334,12 +345,9 @@ __device__ __forceinline__ bool weigh(const float (&s)[2][4], float sc, const Re
             if constexpr (g < NG) {
                 typedef float f2 __attribute__((ext_vector_type(2)));
                 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-                float a = p[0], b = p[1];
-                if constexpr (!PLAIN) {
-                    a *= factor[g];
-                    b *= factor[g];
-                }
-                const f2 y = {__builtin_fmaf(a, (float)half_of(vs[0][at / 2], at & 1), 0.0f), __builtin_fmaf(b, (float)half_of(vs[1][at / 2], at & 1), 0.0f)};
+                f2 y = {__builtin_fmaf(p[0], (float)half_of(vs[0][at / 2], at & 1), 0.0f), __builtin_fmaf(p[1], (float)half_of(vs[1][at / 2], at & 1), 0.0f)};
+                // (last: a weight without a value may be large, and infinite times 0 is no number)
+                if constexpr (!PLAIN) y *= factor[g];
                 x[g][r] = __builtin_bit_cast(unsigned, __builtin_convertvector(y, h2));
             }
         };
@@ -380,24 +388,27 @@ __device__ __forceinline__ float over_h(float x, bool sum) {
     const float z = __shfl_xor(x, 32, 64);
     return sum ? x + z : __builtin_fmaxf(x, z);
 }
-// All references of a row raised to what the 32 keys of a lane and the three others of its column ask for, the sums l and O with them.
+// All references of a row raised to what the 32 keys of a lane and the three others of its column ask for, the sums l and O with them.  (The
+// logarithm of a scale of 0 is -infinity: that key does not ask.)
 template <int NG, int CT, class S>
-__device__ __forceinline__ void raise_references(const float (&s)[2][4], float sc, const S (&vs)[2], References<NG>& ref, const EmptyGroups<NG>& groups, float& l,
-                                                 c4f (&o)[CT]) {
-    float most[NG], alpha[NG];
+__device__ __forceinline__ void raise_references(const float (&s)[2][4], float sc, const S (&vs)[2], References<NG>& ref, float& l, c4f (&o)[CT]) {
+    float most[NG], alpha[NG], score = -__builtin_inff();
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) score = __builtin_fmaxf(score, s[j][r] * sc);
+    score = over_h(score, false);
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
         most[g] = -__builtin_inff();
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float scale = __builtin_fmaxf(SMALLEST, (float)half_of(vs[j][(r * NG + g) / 2], (r * NG + g) & 1));
-                most[g] = __builtin_fmaxf(most[g], __builtin_fmaf(s[j][r], sc, __builtin_amdgcn_logf(scale) - RAISE));
-            }
+            for (int r = 0; r < 4; ++r)
+                most[g] = __builtin_fmaxf(most[g], __builtin_fmaf(s[j][r], sc, __builtin_amdgcn_logf((float)half_of(vs[j][(r * NG + g) / 2], (r * NG + g) & 1)) - RAISE));
         most[g] = over_h(most[g], false);
     }
-    l *= ref.raise(most, groups, alpha);
+    l *= ref.raise(most, score, alpha);
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) o[ct] *= alpha[ct * NG / CT];
 }
@@ -468,7 +479,7 @@ struct RowResult {
 // normalized fp32 and the base-2 logarithm of their sums.
 // (Three wavefronts per SIMD where 168 registers are enough: with four scales of 128 channels they are not, 119 us for 117.)
 template <int D, int NG, int QT>
-__global__ void __launch_bounds__(WAVES * 64, QT == 1 && NG * D < 512 ? 3 : 2)
+__global__ void __launch_bounds__(WAVES * 64, (QT == 1 ? NG * D < 512 : D == 64) ? 3 : 2)
 cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides os, float* __restrict__ lse, float* __restrict__ part,
                    float* __restrict__ part_lse, int tiles, int n_splits, int chunk) {
     constexpr int CT = D / 16, STEPS = D / 32 / NG;
@@ -476,9 +487,9 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
     constexpr int MERGE = WAVES * CT * 64 * 16, STAGE = WAVES * (int)sizeof(Lds);
     __shared__ __attribute__((aligned(16))) unsigned char lds[MERGE > STAGE ? MERGE : STAGE];
     __shared__ float s_m[WAVES][16], s_l[WAVES][16];
-    // (32 rows and four scales of 128 channels: no registers for the second tile's queries, which all wavefronts have alike, nor for
-    // addresses from one tile to the next)
-    constexpr bool STAGED = QT == 2 && NG * D == 512;
+    // (32 rows and four scales of 128 channels: no registers for the second tile's queries, which all wavefronts have alike; there, and with 16
+    // rows and two scales where three wavefronts fit on a SIMD, nor for addresses from one tile to the next)
+    constexpr bool STAGED = QT == 2 && NG * D == 512, ADDRESSES_ANEW = STAGED || (QT == 1 && NG == 2);
     __shared__ half8 s_query[STAGED ? D / 32 : 1][64];
     const unsigned thousand = thousands();
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, h = lane >> 4;
@@ -546,7 +557,7 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
         for (int j = 0; j < 4; ++j) ((words*)mine.k)[j * 64 + lane] = tile.k[j];
         wave_order();
         if (k0 + NEXT < k_end) {
-            tile.request(c, head_at, pages, k0 + NEXT, STAGED ? anew(lane) : lane);
+            tile.request(c, head_at, pages, k0 + NEXT, ADDRESSES_ANEW ? anew(lane) : lane);
             pages.look_up(c, table, k0 + 2 * NEXT);
         }
         const int v_key = 16 * (col >> 2) + 4 * h + (col & 3);
@@ -603,13 +614,12 @@ cache4_attn_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStrides 
                 float sum;
                 if (first || weigh<true, NG>(s[i], sc[i], ref[i], vs, w[i], sum) || again) {
                     const scales_t own[2] = {anew(vs[0]), anew(vs[1])};
-                    raise_references<NG>(s[i], sc[i], own, ref[i], groups, l[i], o[i]);
-                    plain = ref[0].alike() && ref[QT - 1].alike();
+                    raise_references<NG>(s[i], sc[i], own, ref[i], l[i], o[i]);
+                    plain = ref[0].alike(groups) && ref[QT - 1].alike(groups);
                     weigh<NG == 1, NG>(s[i], sc[i], ref[i], vs, w[i], sum);
                 }
                 l[i] += sum;
             }
-            groups.fresh = 0;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 // V transposed: channel 16 ct + lane % 16, nibble i of the words: key 16 (i / 4) + 4 h + i % 4
@@ -803,9 +813,9 @@ cache4_attn_few_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStri
                 const float factor = PLAIN ? 1.0f : ldexpf(1.0f, ref.distance(g));
 #pragma unroll
                 for (int r = 0; r < 4; r += 2) {
-                    const float even = PLAIN ? p[r] : p[r] * factor, odd = PLAIN ? p[r + 1] : p[r + 1] * factor;
-                    const f2 y = {__builtin_fmaf(even, (float)half_of(vs[(r * NG + g) / 2], (r * NG + g) & 1), 0.0f),
-                                  __builtin_fmaf(odd, (float)half_of(vs[((r + 1) * NG + g) / 2], ((r + 1) * NG + g) & 1), 0.0f)};
+                    f2 y = {__builtin_fmaf(p[r], (float)half_of(vs[(r * NG + g) / 2], (r * NG + g) & 1), 0.0f),
+                            __builtin_fmaf(p[r + 1], (float)half_of(vs[((r + 1) * NG + g) / 2], ((r + 1) * NG + g) & 1), 0.0f)};
+                    if constexpr (!PLAIN) y *= factor;
                     x[g][r / 2] = __builtin_bit_cast(unsigned, __builtin_convertvector(y, h2));
                 }
                 top = max3_pairs(top, x[g][0], x[g][1]);
@@ -813,23 +823,26 @@ cache4_attn_few_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStri
             return __builtin_amdgcn_ballot_w64(sum > P_LIMIT || half_of(top, 0) > W_LIMIT || half_of(top, 1) > W_LIMIT) != 0ull;
         };
         if (__builtin_expect(weights(std::true_type{}) || !plain, 0)) {
-            float most[NG], alpha[NG];
+            const auto over_keys = [](float x) {
+                x = __builtin_fmaxf(x, __shfl_xor(x, 4, 64));
+                return over_h(__builtin_fmaxf(x, __shfl_xor(x, 8, 64)), false);
+            };
+            float most[NG], alpha[NG], score = -__builtin_inff();
+#pragma unroll
+            for (int r = 0; r < 4; ++r) score = __builtin_fmaxf(score, s[r] * sc);
+            score = over_keys(score);
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 most[g] = -__builtin_inff();
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float scale = __builtin_fmaxf(SMALLEST, (float)half_of(vs[(r * NG + g) / 2], (r * NG + g) & 1));
-                    most[g] = __builtin_fmaxf(most[g], __builtin_fmaf(s[r], sc, __builtin_amdgcn_logf(scale) - RAISE));
-                }
-                most[g] = __builtin_fmaxf(most[g], __shfl_xor(most[g], 4, 64));
-                most[g] = over_h(__builtin_fmaxf(most[g], __shfl_xor(most[g], 8, 64)), false);
+                for (int r = 0; r < 4; ++r)
+                    most[g] = __builtin_fmaxf(most[g], __builtin_fmaf(s[r], sc, __builtin_amdgcn_logf((float)half_of(vs[(r * NG + g) / 2], (r * NG + g) & 1)) - RAISE));
+                most[g] = over_keys(most[g]);
             }
-            l *= ref.raise(most, groups, alpha);
+            l *= ref.raise(most, score, alpha);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) o[ct] *= alpha[ct * NG / CT];
-            plain = ref.alike();
-            groups.fresh = 0;
+            plain = ref.alike(groups);
             weights(std::integral_constant<bool, NG == 1>{});
         }
         l += sum;
@@ -1076,10 +1089,9 @@ cache4_attn_rows_kernel(Cache4 c, CacheQueries q, void* __restrict__ out, RowStr
 #pragma unroll
         for (int i = 0; i < QT; ++i) {
             const scales_t own[2] = {anew(x.vs[0]), anew(x.vs[1])};
-            raise_references<NG>(x.s[i], sc[i], own, ref[i], groups, l[i], o[i]);
+            raise_references<NG>(x.s[i], sc[i], own, ref[i], l[i], o[i]);
         }
-        plain = ref[0].alike() && ref[QT - 1].alike();
-        groups.fresh = 0;
+        plain = ref[0].alike(groups) && ref[QT - 1].alike(groups);
         weighed(x, std::integral_constant<bool, NG == 1>{});
     };
     auto values = [&](const Half& x, const TileStage<D, NG>& now, int u) {
