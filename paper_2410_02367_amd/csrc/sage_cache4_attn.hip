@@ -454,7 +454,8 @@ struct RowResult {
                                          int all_rows) {
         live = live && total != 0.0f;
         norm = live ? 1.0f / total : 0.0f;
-        log_sum = live ? M + __builtin_amdgcn_logf(total) : -__builtin_inff();
+        // (M and the sum's exponent are whole numbers that nearly cancel where V's scales are small: their sum first, without rounding)
+        log_sum = live ? (M + (float)__builtin_amdgcn_frexp_expf(total)) + __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(total)) : -__builtin_inff();
         part_row = ((size_t)at.split * at.slabs + at.slab) * all_rows + row;
         tq = row / share;
         b = at.slab / (q.Hq / share);
